@@ -400,6 +400,77 @@ int peagle_draft_decode_static(const peagle_decode_shape_t* shape, const void* q
                                const int32_t* block_table, const int32_t* ctx_len, void* o, float* lse,
                                int32_t* status, void* stream);
 
+/*
+ * The paged cache between the drafting steps, with its keys and values held in 8 bits: block tables and slot maps from
+ * request lengths (peagle_cache_plan) and storing new tokens (peagle_cache_append_scaled).  A page is 64 tokens of one
+ * request, as above; the block table that the plan leaves serves peagle_draft_decode as well.
+ *
+ * peagle_cache_plan: after it, request c holds the pages of its first ctx_len[c] + new_len[c] tokens.  Pages that it lacks
+ * are taken from the end of a list of free ones, pages that it no longer needs (a request that ended, both lengths 0; a
+ * draft that was rejected) are put on it, and every new token is told its slot.
+ *
+ *   shape        C requests (1 .. 65535), max_pages block-table columns (<= 2^24), n_pages pages in the pools (<= 2^30),
+ *                max_tokens entries of the slot map (<= 2^30); all at least 1
+ *   ctx_len      device, int32 [C]: cached tokens       new_len  device, int32 [C]: tokens to be stored next, >= 0
+ *   pages_held   device, int32 [C]: pages that each request holds, the first of its row of the block table
+ *   pages_held_out   device, int32 [C] (out): the same after the call; may be pages_held
+ *   free_pages   device, int32 [n_pages] (in and out), free_count device, int32 [1]: the free pages, entries [0, free_count)
+ *   free_count_out   device, int32 [1] (out); may be free_count
+ *   block_table  device, int32 [C, max_pages] (in and out): entries of pages taken are written, all others are left
+ *   token_start  device, int32 [C + 1] (out): row of each request's first new token where all of them stand one after
+ *                another, and their number; at most max_tokens
+ *   slots        device, int64 [max_tokens] (out): 64 * page + place in the page of each such row; -1 for a token that gets
+ *                none, and behind the last token
+ *   seq_len      device, int32 [C] (out): ctx_len + new_len where the request is served, ctx_len otherwise
+ *   status       device, int32 [C] (out): 0 served; 1 a length is negative, the sum beyond the table, pages_held outside
+ *                [ceil(ctx_len / 64), max_pages] or the last new row beyond max_tokens; 2 no pages left.  Such a request
+ *                keeps what it holds; its rows (none for a negative new_len) count in token_start and get slots of -1
+ *   workspace    device, >= peagle_cache_plan_workspace_bytes(); contents undefined before and after
+ *
+ * Pages are given back before any are taken, those of the last request first and of each request the last block first, so
+ * that what ends in one call stands on the list as it did before it was taken in one.  They are taken in order of the requests
+ * and blocks; the first request that does not find all it lacks and those after it that lack any get none.  A free_count
+ * outside [0, n_pages] is clamped; page ids outside the pools are passed on to the table, with slots of -1.  Entries of
+ * free_pages at and behind free_count_out are left as they are.
+ */
+typedef struct peagle_plan_shape {
+  int32_t C, max_pages, n_pages, max_tokens;
+} peagle_plan_shape_t;
+size_t peagle_cache_plan_workspace_bytes(const peagle_plan_shape_t* shape);
+int peagle_cache_plan(const peagle_plan_shape_t* shape, const int32_t* ctx_len, const int32_t* new_len,
+                      const int32_t* pages_held, int32_t* pages_held_out, int32_t* free_pages, const int32_t* free_count,
+                      int32_t* free_count_out, int32_t* block_table, int32_t* token_start, int64_t* slots, int32_t* seq_len,
+                      int32_t* status, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Stores new tokens in a cache that is held in 8 bits.  The 64 tokens of a page share one scale per KV head (K and V apart),
+ * a power of two 2^(code - 127) kept as its code (E8M0); a value is its code of the 8-bit type times the scale.
+ *
+ *   shape        n_tokens rows (0 .. 2^28), Hkv heads, D in {64, 128}, n_pages pages, the type, and the distance in elements
+ *                between two tokens' rows of Hkv x D in k_new and v_new (at least Hkv * D, a multiple of 8)
+ *   k_new, v_new   device, bf16, 16-byte aligned
+ *   slots        device, int64 [n_tokens]: 64 * page + place in the page; a token whose slot is outside [0, 64 * n_pages)
+ *                is not stored
+ *   k_pages, v_pages   device, 8-bit [n_pages, Hkv, 64, D] (in and out), 16-byte aligned
+ *   k_scale, v_scale   device, uint8 [n_pages, Hkv] (in and out)
+ *
+ * Consecutive rows with consecutive slots of one page are a run.  A run that begins at place 0 begins the page: its scale is
+ * the smallest power of two, at least 2^-100, that brings the run's largest finite value to the type's largest (448 or 57344)
+ * or below.  A run that begins further on adds to the tokens before it: the scale becomes the larger of that and the page's
+ * own, and where it grows, the tokens before the run are divided by the growth and rounded again (exact but for what becomes
+ * subnormal).  Places behind the run are left as they are and hold no tokens.  Values are rounded to nearest, ties to even;
+ * NaN stays NaN, an infinity becomes NaN (E4M3) or stays (E5M2).  The runs of a call are in pages of their own: of two in
+ * one page it is not defined which scale and values remain.
+ */
+#define PEAGLE_CACHE_E4M3 0 /* 8 bits: sign, 4 of exponent, 3 of fraction; no infinity */
+#define PEAGLE_CACHE_E5M2 1 /* 8 bits: sign, 5 of exponent, 2 of fraction */
+typedef struct peagle_cache_shape {
+  int32_t n_tokens, Hkv, D, n_pages, format;
+  int64_t k_stride, v_stride;
+} peagle_cache_shape_t;
+int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, const void* k_new, const void* v_new, const int64_t* slots,
+                               void* k_pages, void* v_pages, void* k_scale, void* v_scale, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* peagle_strerror(int status);
 

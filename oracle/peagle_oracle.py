@@ -491,3 +491,99 @@ def draft_decode(q_new: np.ndarray, k_new: np.ndarray, v_new: np.ndarray, k_ctx:
         O[:, h, :] = (E / Z) @ vals[:, g, :]
         LSE[h] = (m + np.log(Z))[:, 0]
     return O, LSE
+
+
+# ------------------------------------------------------------------- paged cache between the drafting steps
+
+PAGE_TOKENS = 64
+F8 = {  # 8-bit types of the cache: fraction bits, exponent of the smallest normal value, largest finite value
+    "e4m3": (3, -6, 448.0),
+    "e5m2": (2, -14, 57344.0),
+}
+MIN_SCALE_EXPONENT = -100
+
+
+def f8_round(x: np.ndarray, fmt: str) -> np.ndarray:
+    """x rounded to the values of an 8-bit type, to nearest, ties to even.  Finite |x| are at most the largest value; an
+    infinity becomes NaN in the type that has none."""
+    bits, low, largest = F8[fmt]
+    x = np.asarray(x, dtype=np.float64)
+    fin = np.isfinite(x)
+    assert (np.abs(x[fin]) <= largest).all()
+    step = np.exp2(np.maximum(np.frexp(np.where(fin, x, 0.0))[1] - 1, low) - bits)
+    y = np.where(fin, np.rint(np.where(fin, x, 0.0) / step) * step, x)
+    return np.where(np.isinf(y), np.nan, y) if fmt == "e4m3" else y
+
+
+def scale_exponent(amax: float, fmt: str) -> int:
+    """The smallest e with amax <= largest * 2^e, at least MIN_SCALE_EXPONENT."""
+    e = MIN_SCALE_EXPONENT
+    while amax > F8[fmt][2] * 2.0 ** e:
+        e += 1
+    return e
+
+
+def cache_append(x: np.ndarray, slots: np.ndarray, pages: np.ndarray, exps: np.ndarray, fmt: str) -> None:
+    """Stores x [n, H, D] at `slots` (page * 64 + place; outside the pool: not stored), in place.  pages [n_pages, H, 64, D]:
+    the values of the 8-bit type that the cache holds, before the page's scale 2^exps [n_pages, H].  Consecutive rows with
+    consecutive slots of one page are a run: at place 0 it begins the page, further on it adds to it, and the tokens before
+    it are rounded again where the scale has to grow."""
+    slots = np.asarray(slots, dtype=np.int64)
+    n, limit = len(slots), len(pages) * PAGE_TOKENS
+    t = 0
+    while t < n:
+        if not 0 <= slots[t] < limit:
+            t += 1
+            continue
+        end = t + 1
+        while end < n and slots[end] == slots[end - 1] + 1 and slots[end] % PAGE_TOKENS:
+            end += 1
+        page, at = divmod(int(slots[t]), PAGE_TOKENS)
+        for h in range(x.shape[1]):
+            run = np.asarray(x[t:end, h], dtype=np.float64)
+            fin = np.abs(run[np.isfinite(run)])
+            e = scale_exponent(fin.max() if fin.size else 0.0, fmt)
+            if at:
+                e = max(e, int(exps[page, h]))
+                pages[page, h, :at] = f8_round(pages[page, h, :at] * 2.0 ** (int(exps[page, h]) - e), fmt)
+            pages[page, h, at:at + end - t] = f8_round(run * 2.0 ** -e, fmt)
+            exps[page, h] = e
+        t = end
+
+
+def cache_plan(ctx_len, new_len, held, free_pages, free_count: int, table, max_tokens: int) -> Dict[str, np.ndarray]:
+    """Request by request: pages that a request no longer needs go on the list (last request and block first), then each takes
+    what it lacks off its end; slots of the new tokens.  Returns all results; the arguments are left as they are."""
+    ctx, new, held = (np.asarray(a, dtype=np.int64) for a in (ctx_len, new_len, held))
+    free, table = np.array(free_pages), np.array(table)
+    C, max_pages, n_pages = len(ctx), table.shape[1], len(free)
+    pages = lambda tokens: -(-int(tokens) // PAGE_TOKENS)
+    start, status, want = [0], [], []
+    for c in range(C):
+        start.append(start[-1] + max(int(new[c]), 0))
+        good = ctx[c] >= 0 and new[c] >= 0 and ctx[c] + new[c] <= PAGE_TOKENS * max_pages and pages(ctx[c]) <= held[c] <= max_pages
+        status.append(0 if good and start[-1] <= max_tokens else 1)
+        want.append(pages(ctx[c] + new[c]) if status[c] == 0 else int(held[c]))
+    stack = [int(p) for p in free[:min(max(int(free_count), 0), n_pages)]]
+    for c in reversed(range(C)):
+        for b in reversed(range(want[c], int(held[c]))):
+            if len(stack) < n_pages:
+                free[len(stack)] = table[c, b]
+                stack.append(int(table[c, b]))
+    slots, out = np.full(max_tokens, -1, dtype=np.int64), False
+    for c in range(C):
+        lacks = want[c] - int(held[c])
+        if status[c] == 0 and lacks > 0:
+            out = out or lacks > len(stack)
+            if out:
+                status[c], want[c] = 2, int(held[c])
+            for b in range(int(held[c]), want[c]):
+                table[c, b] = stack.pop()
+        if status[c] == 0:
+            for j in range(int(new[c])):
+                b, place = divmod(int(ctx[c]) + j, PAGE_TOKENS)
+                if 0 <= table[c, b] < n_pages:
+                    slots[start[c] + j] = int(table[c, b]) * PAGE_TOKENS + place
+    return {"pages_held": np.array(want), "free_pages": free, "free_count": np.array([len(stack)]), "block_table": table,
+            "token_start": np.minimum(start, max_tokens), "slots": slots,
+            "seq_len": np.where(np.array(status) == 0, ctx + new, ctx), "status": np.array(status)}

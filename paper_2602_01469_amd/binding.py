@@ -36,6 +36,15 @@ class _DecodeShapeC(C.Structure):
                 ("scale", C.c_float), ("n_pages", C.c_int32), ("max_pages", C.c_int32)]
 
 
+class _PlanShapeC(C.Structure):
+    _fields_ = [("C", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("max_tokens", C.c_int32)]
+
+
+class _CacheShapeC(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("n_pages", C.c_int32), ("format", C.c_int32),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
 EXPORTS = [
     "peagle_build_tilemap", "peagle_tilemap_destroy", "peagle_tilemap_info", "peagle_tilemap_expand_rows",
     "peagle_tilemap_classes", "peagle_workspace_bytes", "peagle_attn_fwd", "peagle_attn_bwd",
@@ -46,6 +55,7 @@ EXPORTS = [
     "peagle_rope_shared_workspace_bytes", "peagle_attn_step_rope_shared",
     "peagle_draft_decode_splits", "peagle_draft_decode_workspace_bytes", "peagle_draft_decode",
     "peagle_draft_decode_static",
+    "peagle_cache_plan_workspace_bytes", "peagle_cache_plan", "peagle_cache_append_scaled",
     "peagle_attn_step_profiled", "peagle_measure_mfma_ceiling", "peagle_measure_mfma_ceiling_random", "peagle_device_info", "peagle_strerror",
 ]
 
@@ -133,6 +143,12 @@ def load_library():
     lib.peagle_draft_decode.restype = C.c_int
     lib.peagle_draft_decode_static.argtypes = [C.POINTER(_DecodeShapeC), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.peagle_draft_decode_static.restype = C.c_int
+    lib.peagle_cache_plan_workspace_bytes.argtypes = [C.POINTER(_PlanShapeC)]
+    lib.peagle_cache_plan_workspace_bytes.restype = sz
+    lib.peagle_cache_plan.argtypes = [C.POINTER(_PlanShapeC), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.peagle_cache_plan.restype = C.c_int
+    lib.peagle_cache_append_scaled.argtypes = [C.POINTER(_CacheShapeC), vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.peagle_cache_append_scaled.restype = C.c_int
     lib.peagle_measure_mfma_ceiling.argtypes = [vp, C.POINTER(C.c_float)]
     lib.peagle_measure_mfma_ceiling.restype = C.c_int
     lib.peagle_measure_mfma_ceiling_random.argtypes = [vp, C.POINTER(C.c_float)]
@@ -561,6 +577,113 @@ def peagle_draft_decode_static(shape: DecodeShape, q_new, k_new, v_new, k_pages,
         _ptr(lse, "lse", f32, (s.C, s.Hq, s.K)), _ptr(status, "status", i32, (s.C,)), _stream_ptr(stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_draft_decode_static")
+
+
+class PlanShape:
+    """Shape of one plan of the paged cache: C requests, a block table of max_pages columns, n_pages pages, at most
+    max_tokens new tokens."""
+
+    def __init__(self, C_: int, max_pages: int, n_pages: int, max_tokens: int):
+        self.C, self.max_pages, self.n_pages, self.max_tokens = C_, max_pages, n_pages, max_tokens
+
+    def c(self):
+        return C.byref(_PlanShapeC(self.C, self.max_pages, self.n_pages, self.max_tokens))
+
+
+def peagle_cache_plan_workspace_bytes(shape: PlanShape) -> int:
+    n = int(load_library().peagle_cache_plan_workspace_bytes(shape.c()))
+    if n == 0:
+        raise PeagleError(-3, "peagle_cache_plan_workspace_bytes")
+    return n
+
+
+def _on_current_device(**tensors) -> None:
+    """The call runs on the current device's stream: its tensors have to be that device's."""
+    import torch
+    dev = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{name}: lives on {t.device}, the current device is cuda:{dev}")
+
+
+def peagle_cache_plan(shape: PlanShape, ctx_len, new_len, pages_held, free_pages, free_count, block_table, token_start, slots,
+                      seq_len, status, workspace, pages_held_out=None, free_count_out=None, stream=None) -> None:
+    """Pages and slots of each request's next tokens; pages_held and free_count are updated in place unless the results are
+    given tensors of their own."""
+    import torch
+    i32, s = torch.int32, shape
+    if pages_held_out is None:
+        pages_held_out = pages_held
+    if free_count_out is None:
+        free_count_out = free_count
+    if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace: expected a contiguous uint8 GPU tensor")
+    per_request = (s.C,)
+    args = [_ptr(ctx_len, "ctx_len", i32, per_request), _ptr(new_len, "new_len", i32, per_request),
+            _ptr(pages_held, "pages_held", i32, per_request), _ptr(pages_held_out, "pages_held_out", i32, per_request),
+            _ptr(free_pages, "free_pages", i32, (s.n_pages,)), _ptr(free_count, "free_count", i32, (1,)),
+            _ptr(free_count_out, "free_count_out", i32, (1,)), _ptr(block_table, "block_table", i32, (s.C, s.max_pages)),
+            _ptr(token_start, "token_start", i32, (s.C + 1,)), _ptr(slots, "slots", torch.int64, (s.max_tokens,)),
+            _ptr(seq_len, "seq_len", i32, per_request), _ptr(status, "status", i32, per_request)]
+    _on_current_device(ctx_len=ctx_len, new_len=new_len, pages_held=pages_held, pages_held_out=pages_held_out,
+                       free_pages=free_pages, free_count=free_count, free_count_out=free_count_out, block_table=block_table,
+                       token_start=token_start, slots=slots, seq_len=seq_len, status=status, workspace=workspace)
+    rc = load_library().peagle_cache_plan(s.c(), *args, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise PeagleError(rc, "peagle_cache_plan")
+
+
+class CacheShape:
+    """Shape of an append to a paged cache held in 8 bits: n_tokens new tokens; the pools' type says which one it is."""
+
+    def __init__(self, n_tokens: int, Hkv: int, D: int, n_pages: int):
+        self.n_tokens, self.Hkv, self.D, self.n_pages = n_tokens, Hkv, D, n_pages
+
+
+CACHE_E4M3, CACHE_E5M2 = 0, 1
+
+
+def _cache_pools(k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: int, D: int):
+    """Pointers of an 8-bit cache's pools and scales, and its format."""
+    import torch
+    formats = {torch.float8_e4m3fn: CACHE_E4M3, torch.float8_e5m2: CACHE_E5M2}
+    if k_pages.dtype not in formats:
+        raise TypeError(f"k_pages: expected torch.float8_e4m3fn or torch.float8_e5m2, got {k_pages.dtype}")
+    if v_pages.dtype != k_pages.dtype:
+        raise TypeError(f"v_pages: expected {k_pages.dtype}, got {v_pages.dtype}")
+    pool, e8 = (n_pages, Hkv, 64, D), torch.float8_e8m0fnu
+    return formats[k_pages.dtype], [_ptr(k_pages, "k_pages", k_pages.dtype, pool), _ptr(v_pages, "v_pages", k_pages.dtype, pool),
+                                    _ptr(k_scale, "k_scale", e8, (n_pages, Hkv)), _ptr(v_scale, "v_scale", e8, (n_pages, Hkv))]
+
+
+def _rows_ptr(t, name: str, dtype, shape):
+    """Device pointer and row distance (elements) of a tensor whose rows are whole but may stand apart."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must live on the GPU")
+    n, H, D = shape
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    return t.data_ptr(), t.stride(0) if n > 1 else H * D
+
+
+def peagle_cache_append_scaled(shape: CacheShape, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream=None) -> None:
+    """Stores k_new, v_new [n_tokens, Hkv, D] (a token's heads contiguous, tokens any multiple of 8 elements apart) at `slots`."""
+    import torch
+    s = shape
+    fmt, pools = _cache_pools(k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    rows = (s.n_tokens, s.Hkv, s.D)
+    k, k_stride = _rows_ptr(k_new, "k_new", torch.bfloat16, rows)
+    v, v_stride = _rows_ptr(v_new, "v_new", torch.bfloat16, rows)
+    at = _ptr(slots, "slots", torch.int64, (s.n_tokens,))
+    _on_current_device(k_new=k_new, v_new=v_new, slots=slots, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale)
+    c = _CacheShapeC(s.n_tokens, s.Hkv, s.D, s.n_pages, fmt, k_stride, v_stride)
+    rc = load_library().peagle_cache_append_scaled(C.byref(c), k, v, at, *pools, _stream_ptr(stream))
+    if rc != 0:
+        raise PeagleError(rc, "peagle_cache_append_scaled")
 
 
 def peagle_measure_mfma_ceiling(stream=None, random_operands: bool = False) -> float:

@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "attn_kernels.h"
+#include "cache_kernels.h"
 #include "peagle.h"
 #include "peagle_bench.h"
 #include "tilemap.h"
@@ -674,6 +675,87 @@ extern "C" int peagle_draft_decode_static(const peagle_decode_shape_t* shape, co
   if (src != PEAGLE_OK) return src;
   // Every partial record the merge reads is written by this call's first launch: nothing has to start at zero.
   return decode_impl(shape, w, q_new, k_new, v_new, k_pages, v_pages, block_table, ctx_len, o, lse, status, ws, stream);
+}
+
+namespace {
+
+int check_plan(const peagle_plan_shape_t* s) {
+  if (!s) return PEAGLE_ENULL;
+  if (s->C < 1 || s->max_pages < 1 || s->n_pages < 1 || s->max_tokens < 1) return PEAGLE_EINVAL;
+  if (s->C > 65535 || s->max_pages > (1 << 24)) return PEAGLE_EUNSUPPORTED;         // as the drafting step
+  if (s->n_pages > (1 << 30) || s->max_tokens > (1 << 30)) return PEAGLE_EUNSUPPORTED;  // sums of two must fit an int
+  return PEAGLE_OK;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+
+extern "C" size_t peagle_cache_plan_workspace_bytes(const peagle_plan_shape_t* shape) {
+  return check_plan(shape) == PEAGLE_OK ? align256((size_t)shape->C * sizeof(peagle::PlanRecord)) : 0;
+}
+
+extern "C" int peagle_cache_plan(const peagle_plan_shape_t* shape, const int32_t* ctx_len, const int32_t* new_len,
+                                 const int32_t* pages_held, int32_t* pages_held_out, int32_t* free_pages,
+                                 const int32_t* free_count, int32_t* free_count_out, int32_t* block_table, int32_t* token_start,
+                                 int64_t* slots, int32_t* seq_len, int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_plan(shape);
+  if (rc != PEAGLE_OK) return rc;
+  if (!ctx_len || !new_len || !pages_held || !pages_held_out || !free_pages || !free_count || !free_count_out || !block_table ||
+      !token_start || !slots || !seq_len || !status)
+    return PEAGLE_ENULL;
+  if (!workspace || ws_bytes < peagle_cache_plan_workspace_bytes(shape)) return PEAGLE_EWORKSPACE;
+  peagle::PlanParams p{};
+  p.ctx_len = ctx_len;
+  p.new_len = new_len;
+  p.held = pages_held;
+  p.held_out = pages_held_out;
+  p.free_pages = free_pages;
+  p.free_count = free_count;
+  p.free_count_out = free_count_out;
+  p.block_table = block_table;
+  p.token_start = token_start;
+  p.slots = slots;
+  p.seq_len = seq_len;
+  p.status = status;
+  p.records = (peagle::PlanRecord*)workspace;
+  p.C = shape->C;
+  p.max_pages = shape->max_pages;
+  p.n_pages = shape->n_pages;
+  p.max_tokens = shape->max_tokens;
+  return peagle::launch_cache_plan(p, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK : PEAGLE_EHIP;
+}
+
+extern "C" int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, const void* k_new, const void* v_new,
+                                          const int64_t* slots, void* k_pages, void* v_pages, void* k_scale, void* v_scale,
+                                          void* stream) {
+  if (!shape) return PEAGLE_ENULL;
+  const peagle_cache_shape_t& s = *shape;
+  if (s.n_tokens < 0 || s.Hkv < 1 || s.n_pages < 1) return PEAGLE_EINVAL;
+  if (s.D != 64 && s.D != 128) return PEAGLE_EUNSUPPORTED;
+  if (s.format != PEAGLE_CACHE_E4M3 && s.format != PEAGLE_CACHE_E5M2) return PEAGLE_EUNSUPPORTED;
+  if (s.n_tokens > (1 << 28) || s.Hkv > 65535 || s.n_pages > (1 << 30)) return PEAGLE_EUNSUPPORTED;  // grid dimensions
+  const int64_t row = (int64_t)s.Hkv * s.D;
+  if (s.k_stride < row || s.v_stride < row || s.k_stride % 8 != 0 || s.v_stride % 8 != 0) return PEAGLE_EINVAL;
+  if (!k_pages || !v_pages || !k_scale || !v_scale) return PEAGLE_ENULL;
+  if (s.n_tokens == 0) return PEAGLE_OK;
+  if (!k_new || !v_new || !slots) return PEAGLE_ENULL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages)) return PEAGLE_EINVAL;
+  peagle::AppendParams p{};
+  p.k_new = (const __bf16*)k_new;
+  p.v_new = (const __bf16*)v_new;
+  p.slots = slots;
+  p.k_pages = (uint8_t*)k_pages;
+  p.v_pages = (uint8_t*)v_pages;
+  p.k_scale = (uint8_t*)k_scale;
+  p.v_scale = (uint8_t*)v_scale;
+  p.k_stride = s.k_stride;
+  p.v_stride = s.v_stride;
+  p.n_tokens = s.n_tokens;
+  p.Hkv = s.Hkv;
+  p.n_pages = s.n_pages;
+  return peagle::launch_cache_append(p, s.D, s.format == PEAGLE_CACHE_E5M2, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK
+                                                                                                              : PEAGLE_EHIP;
 }
 
 extern "C" int peagle_measure_mfma_ceiling(void* stream, float* tflops) {
