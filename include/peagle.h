@@ -402,8 +402,9 @@ int peagle_draft_decode_static(const peagle_decode_shape_t* shape, const void* q
 
 /*
  * The paged cache between the drafting steps, with its keys and values held in 8 bits: block tables and slot maps from
- * request lengths (peagle_cache_plan) and storing new tokens (peagle_cache_append_scaled).  A page is 64 tokens of one
- * request, as above; the block table that the plan leaves serves peagle_draft_decode as well.
+ * request lengths (peagle_cache_plan), storing new tokens (peagle_cache_append_scaled) and the drafting step that reads
+ * such a cache (peagle_draft_decode_scaled).  A page is 64 tokens of one request, as above; the block table that the plan
+ * leaves serves peagle_draft_decode as well.
  *
  * peagle_cache_plan: after it, request c holds the pages of its first ctx_len[c] + new_len[c] tokens.  Pages that it lacks
  * are taken from the end of a list of free ones, pages that it no longer needs (a request that ended, both lengths 0; a
@@ -470,6 +471,19 @@ typedef struct peagle_cache_shape {
 } peagle_cache_shape_t;
 int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, const void* k_new, const void* v_new, const int64_t* slots,
                                void* k_pages, void* v_pages, void* k_scale, void* v_scale, void* stream);
+
+/*
+ * peagle_draft_decode on such a cache: the same shape, arguments and results, with 8-bit pools (16-byte aligned) of the type
+ * `format` and their scales k_scale, v_scale (device, uint8 [n_pages, Hkv]; any code, 255 is NaN).  The new positions' keys
+ * and values are bf16, as there.  Codes and scales become bf16 without rounding; scores, row sums and outputs are summed in
+ * fp32, probabilities are rounded to bf16 before they weigh the values.
+ */
+int32_t peagle_draft_decode_scaled_splits(const peagle_decode_shape_t* shape);
+size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode_shape_t* shape);
+int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,
+                               const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale,
+                               const void* v_scale, const int32_t* block_table, const int32_t* ctx_len, void* o, float* lse,
+                               int32_t* status, void* workspace, size_t ws_bytes, void* stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* peagle_strerror(int status);

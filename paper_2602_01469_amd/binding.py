@@ -56,6 +56,7 @@ EXPORTS = [
     "peagle_draft_decode_splits", "peagle_draft_decode_workspace_bytes", "peagle_draft_decode",
     "peagle_draft_decode_static",
     "peagle_cache_plan_workspace_bytes", "peagle_cache_plan", "peagle_cache_append_scaled",
+    "peagle_draft_decode_scaled_splits", "peagle_draft_decode_scaled_workspace_bytes", "peagle_draft_decode_scaled",
     "peagle_attn_step_profiled", "peagle_measure_mfma_ceiling", "peagle_measure_mfma_ceiling_random", "peagle_device_info", "peagle_strerror",
 ]
 
@@ -149,6 +150,13 @@ def load_library():
     lib.peagle_cache_plan.restype = C.c_int
     lib.peagle_cache_append_scaled.argtypes = [C.POINTER(_CacheShapeC), vp, vp, vp, vp, vp, vp, vp, vp]
     lib.peagle_cache_append_scaled.restype = C.c_int
+    lib.peagle_draft_decode_scaled_splits.argtypes = [C.POINTER(_DecodeShapeC)]
+    lib.peagle_draft_decode_scaled_splits.restype = i32
+    lib.peagle_draft_decode_scaled_workspace_bytes.argtypes = [C.POINTER(_DecodeShapeC)]
+    lib.peagle_draft_decode_scaled_workspace_bytes.restype = sz
+    lib.peagle_draft_decode_scaled.argtypes = [C.POINTER(_DecodeShapeC), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
+                                               vp]
+    lib.peagle_draft_decode_scaled.restype = C.c_int
     lib.peagle_measure_mfma_ceiling.argtypes = [vp, C.POINTER(C.c_float)]
     lib.peagle_measure_mfma_ceiling.restype = C.c_int
     lib.peagle_measure_mfma_ceiling_random.argtypes = [vp, C.POINTER(C.c_float)]
@@ -684,6 +692,38 @@ def peagle_cache_append_scaled(shape: CacheShape, k_new, v_new, slots, k_pages, 
     rc = load_library().peagle_cache_append_scaled(C.byref(c), k, v, at, *pools, _stream_ptr(stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_cache_append_scaled")
+
+
+def peagle_draft_decode_scaled_splits(shape: DecodeShape) -> int:
+    return int(load_library().peagle_draft_decode_scaled_splits(shape.c()))
+
+
+def peagle_draft_decode_scaled_workspace_bytes(shape: DecodeShape) -> int:
+    n = int(load_library().peagle_draft_decode_scaled_workspace_bytes(shape.c()))
+    if n == 0:
+        raise PeagleError(-3, "peagle_draft_decode_scaled_workspace_bytes")
+    return n
+
+
+def peagle_draft_decode_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages, v_pages, k_scale, v_scale, block_table, ctx_len, o,
+                               lse, status, workspace, stream=None) -> None:
+    """peagle_draft_decode on a cache held in 8 bits: pools of torch.float8_e4m3fn or torch.float8_e5m2, scales of
+    torch.float8_e8m0fnu."""
+    import torch
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    s = shape
+    if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace: expected a contiguous uint8 GPU tensor")
+    fmt, pools = _cache_pools(k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    new = (s.C, s.K, s.Hkv, s.D)
+    args = [_ptr(q_new, "q_new", bf, (s.C, s.K, s.Hq, s.D)), _ptr(k_new, "k_new", bf, new), _ptr(v_new, "v_new", bf, new), *pools,
+            _ptr(block_table, "block_table", i32, (s.C, s.max_pages)), _ptr(ctx_len, "ctx_len", i32, (s.C,)),
+            _ptr(o, "o", bf, (s.C, s.K, s.Hq, s.D)), _ptr(lse, "lse", f32, (s.C, s.Hq, s.K)), _ptr(status, "status", i32, (s.C,))]
+    _on_current_device(q_new=q_new, k_new=k_new, v_new=v_new, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale,
+                       block_table=block_table, ctx_len=ctx_len, o=o, lse=lse, status=status, workspace=workspace)
+    rc = load_library().peagle_draft_decode_scaled(s.c(), fmt, *args, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise PeagleError(rc, "peagle_draft_decode_scaled")
 
 
 def peagle_measure_mfma_ceiling(stream=None, random_operands: bool = False) -> float:

@@ -591,15 +591,13 @@ extern "C" size_t peagle_draft_decode_workspace_bytes(const peagle_decode_shape_
 
 namespace {
 
-int decode_impl(const peagle_decode_shape_t* shape, const DecodeWs& w, const void* q_new, const void* k_new,
-                const void* v_new, const void* k_pages, const void* v_pages, const int32_t* block_table,
-                const int32_t* ctx_len, void* o, float* lse, int32_t* status, void* workspace, void* stream) {
+peagle::DecodeParams decode_params(const peagle_decode_shape_t* shape, const DecodeWs& w, const void* q_new, const void* k_new,
+                                   const void* v_new, const int32_t* block_table, const int32_t* ctx_len, void* o, float* lse,
+                                   int32_t* status, void* workspace) {
   peagle::DecodeParams p{};
   p.q_new = (const __bf16*)q_new;
   p.k_new = (const __bf16*)k_new;
   p.v_new = (const __bf16*)v_new;
-  p.k_pages = (const __bf16*)k_pages;
-  p.v_pages = (const __bf16*)v_pages;
   p.block_table = block_table;
   p.ctx_len = ctx_len;
   p.o = (__bf16*)o;
@@ -616,6 +614,15 @@ int decode_impl(const peagle_decode_shape_t* shape, const DecodeWs& w, const voi
   p.n_splits = w.n_splits;
   p.rows_pad = w.rows_pad;
   p.c_log2 = shape->scale * 1.4426950408889634f;
+  return p;
+}
+
+int decode_impl(const peagle_decode_shape_t* shape, const DecodeWs& w, const void* q_new, const void* k_new,
+                const void* v_new, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                const int32_t* ctx_len, void* o, float* lse, int32_t* status, void* workspace, void* stream) {
+  peagle::DecodeParams p = decode_params(shape, w, q_new, k_new, v_new, block_table, ctx_len, o, lse, status, workspace);
+  p.k_pages = (const __bf16*)k_pages;
+  p.v_pages = (const __bf16*)v_pages;
   return peagle::launch_draft_decode(p, shape->D, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK : PEAGLE_EHIP;
 }
 
@@ -756,6 +763,53 @@ extern "C" int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, con
   p.n_pages = s.n_pages;
   return peagle::launch_cache_append(p, s.D, s.format == PEAGLE_CACHE_E5M2, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK
                                                                                                               : PEAGLE_EHIP;
+}
+
+// The drafting step on a cache held in 8 bits: partial records as above, for the pieces that the launch takes.
+namespace {
+
+DecodeWs decode_scaled_ws(const peagle_decode_shape_t* s) {
+  DecodeWs w;
+  w.n_splits = peagle::draft_scaled_pieces((int64_t)s->C * s->Hkv, s->max_pages, s->D);
+  w.rows_pad = (s->K * (s->Hq / s->Hkv) + 31) / 32 * 32;
+  const size_t recs = w.n_splits > 1 ? (size_t)s->C * s->Hkv * w.n_splits : 0;
+  w.o_off = 0;
+  w.ml_off = align256(recs * w.rows_pad * s->D * sizeof(float));
+  w.total = w.ml_off + align256(recs * 3 * w.rows_pad * sizeof(float)) + 256;  // (never 0, which means a shape that is refused)
+  return w;
+}
+
+}  // namespace
+
+extern "C" int32_t peagle_draft_decode_scaled_splits(const peagle_decode_shape_t* shape) {
+  return check_decode(shape) == PEAGLE_OK ? decode_scaled_ws(shape).n_splits : -1;
+}
+
+extern "C" size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode_shape_t* shape) {
+  return check_decode(shape) == PEAGLE_OK ? decode_scaled_ws(shape).total : 0;
+}
+
+extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,
+                                          const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale,
+                                          const void* v_scale, const int32_t* block_table, const int32_t* ctx_len, void* o,
+                                          float* lse, int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_decode(shape);
+  if (rc != PEAGLE_OK) return rc;
+  if (format != PEAGLE_CACHE_E4M3 && format != PEAGLE_CACHE_E5M2) return PEAGLE_EUNSUPPORTED;
+  if (!q_new || !k_new || !v_new || !k_pages || !v_pages || !k_scale || !v_scale || !block_table || !ctx_len || !o || !lse)
+    return PEAGLE_ENULL;
+  if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o))
+    return PEAGLE_EINVAL;
+  const DecodeWs w = decode_scaled_ws(shape);
+  if (!workspace || ws_bytes < w.total) return PEAGLE_EWORKSPACE;
+  peagle::ScaledDecodeParams p{};
+  p.d = decode_params(shape, w, q_new, k_new, v_new, block_table, ctx_len, o, lse, status, workspace);
+  p.k_pages = (const uint8_t*)k_pages;
+  p.v_pages = (const uint8_t*)v_pages;
+  p.k_scale = (const uint8_t*)k_scale;
+  p.v_scale = (const uint8_t*)v_scale;
+  return peagle::launch_draft_scaled(p, shape->D, format == PEAGLE_CACHE_E5M2, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK
+                                                                                                                 : PEAGLE_EHIP;
 }
 
 extern "C" int peagle_measure_mfma_ceiling(void* stream, float* tflops) {

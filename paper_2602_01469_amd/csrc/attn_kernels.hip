@@ -9,6 +9,7 @@
 // registers <-> rows).  Operands whose contraction index is not contiguous in memory are read
 // from LDS with ds_read_b64_tr_b16.
 #include "attn_kernels.h"
+#include "attn_util.h"
 #include "mfma_util.h"
 #include "rope_util.h"
 
@@ -20,7 +21,6 @@ namespace peagle {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 // How far the running reference max may lag, log2 units (moving it costs a pass over the accumulators).  A drafting step keeps
 // it closer: the key that is the reference has a probability of exactly 1, unrounded, and the fewer pieces a context is cut
 // into, the fewer references it starts.  Error against 64 bits, rel-L2, mean of 31 batches (and the worst of them against the
@@ -32,15 +32,6 @@ constexpr float kNegInit = -1.0e30f;
 // Bits of a 32-key mask word (already shifted right by 4g) that belong to the keys a lane holds in the
 // C layout of a transposed score block: keys 8*(i/4) + 4g + i%4, i = 0..15.
 constexpr uint32_t kLaneKeyBits = 0x0f0f0f0fu;
-
-// n / d and, in its place, n % d; n wave-uniform and below 2^31 (see Divisor).
-__device__ __forceinline__ int split_by(int& n, const Divisor& d) {
-  const uint32_t q = (uint32_t)(((uint64_t)(uint32_t)n * d.mul) >> d.shift);
-  n -= (int)(q * d.d);
-  return (int)q;
-}
-// x / d for x < 128, r = small_reciprocal(d)
-__device__ __forceinline__ int small_quotient(int x, uint32_t r) { return (int)(__umul24((uint32_t)x, r) >> 16); }
 
 // Token (row of the [T, H, D] tensors) of key `row` of key tile `kt`; false if that key does not
 // exist in a length-L problem.
@@ -89,9 +80,6 @@ __device__ __forceinline__ bool row_token(const DeviceTileMap& tm, int rt, int r
   return a < tm.A && i < L;
 }
 
-__device__ __forceinline__ uint4 ld16(const __bf16* p) { return *reinterpret_cast<const uint4*>(p); }
-__device__ __forceinline__ bf16x8 as_frag(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
-
 // Entry `e` of a tile list, made wave-uniform (the index is uniform; this lets branches on the
 // entry be scalar).  Lists are read two iterations ahead of their use: fetch_entry() starts the
 // load early in an iteration, take_entry() - called after the iteration's barrier - moves the
@@ -132,13 +120,6 @@ struct KeyTileLds {
   __device__ __forceinline__ uint32_t k(int slot) const { return base + (uint32_t)slot * (2u * kKeysPerTile * D * 2); }
   __device__ __forceinline__ uint32_t v(int slot) const { return k(slot) + kKeysPerTile * D * 2; }
 };
-
-// The lane's number, computed anew where it stands: what is derived from it takes no register before and after.
-__device__ __forceinline__ int lane_id() {
-  int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-  asm volatile("" : "+v"(l));
-  return l;
-}
 
 // Key tiles straight into their swizzled LDS images (K and V): wave w of NW fills the 1 KiB blocks w, w + NW, ...; lane l of
 // block b owns LDS bytes [1024 b + 16 l, +16), i.e. tile row b*(512/D) + l/(D/8) and physical chunk l%(D/8), and fetches the
@@ -392,26 +373,10 @@ __device__ __forceinline__ float add_delta8(float dl, bf16x8 dof, bf16x8 of) {
   return dl;
 }
 
-// Bit `pos` of w selects x, otherwise -inf.
-__device__ __forceinline__ float mask_sel(float x, uint32_t w, int pos) {
-  return ((w >> pos) & 1u) ? x : -__builtin_inff();
-}
-
 // x where bit `pos` of w is set, otherwise 0 (whatever x is: the exponential of a score that the row does not see may be infinite).
 __device__ __forceinline__ float mask_zero(float x, uint32_t w, int pos) {
   const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)w, pos, 1);
   return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & keep);
-}
-
-__device__ __forceinline__ float max16(const f32x16& s) {
-  float a = __builtin_fmaxf(__builtin_fmaxf(s[0], s[1]), s[2]);
-  float b = __builtin_fmaxf(__builtin_fmaxf(s[3], s[4]), s[5]);
-  float c = __builtin_fmaxf(__builtin_fmaxf(s[6], s[7]), s[8]);
-  float d = __builtin_fmaxf(__builtin_fmaxf(s[9], s[10]), s[11]);
-  float e = __builtin_fmaxf(__builtin_fmaxf(s[12], s[13]), s[14]);
-  a = __builtin_fmaxf(__builtin_fmaxf(a, b), c);
-  d = __builtin_fmaxf(__builtin_fmaxf(d, e), s[15]);
-  return __builtin_fmaxf(a, d);
 }
 
 // Online-softmax update for one 32-key block of one head.  On entry s holds raw q.k of the
@@ -3107,7 +3072,10 @@ hipError_t launch_draft_decode(const DecodeParams& pin, int D, hipStream_t strea
   };
   p.n_splits == 1 ? go(std::true_type{}) : go(std::false_type{});
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_splits == 1) return e;
+  return e != hipSuccess || p.n_splits == 1 ? e : launch_draft_combine(p, D, stream);
+}
+
+hipError_t launch_draft_combine(const DecodeParams& p, int D, hipStream_t stream) {
   // threads per row and splits per thread: n_splits is at most 32
   auto merge = [&](auto kernel, int rows_per_wave) {
     const int per_block = 4 * rows_per_wave;

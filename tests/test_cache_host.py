@@ -135,3 +135,35 @@ def test_binding_refuses_tensors_that_are_not_what_the_shape_says():
     with pytest.raises(TypeError, match="workspace"):
         pe.peagle_cache_plan(plan, i32(2), i32(2), i32(2), i32(4), i32(1), i32(2, 3), i32(3), torch.zeros(5, dtype=torch.int64), i32(2),
                              i32(2), torch.zeros(256, dtype=torch.uint8))
+
+
+def _draft_call(change=None, format_=0, **ptrs):
+    f = {"C": 2, "K": 3, "Hq": 8, "Hkv": 2, "D": 64, "scale": 0.125, "n_pages": 8, "max_pages": 40} | (change or {})
+    c = binding._DecodeShapeC(*f.values())
+    lib = pe.load_library()
+    names = ["q_new", "k_new", "v_new", "k_pages", "v_pages", "k_scale", "v_scale", "block_table", "ctx_len", "o", "lse", "status", "workspace"]
+    need = lib.peagle_draft_decode_scaled_workspace_bytes(C.byref(c))
+    return lib.peagle_draft_decode_scaled(C.byref(c), format_, *[ptrs.get(n, PTR) for n in names], ptrs.get("ws_bytes", need), None)
+
+
+@pytest.mark.parametrize("change,rc", [({"C": 0}, EINVAL), ({"K": 0}, EINVAL), ({"Hkv": 0}, EINVAL), ({"Hkv": 3}, EINVAL), ({"n_pages": 0}, EINVAL),
+                                       ({"max_pages": 0}, EINVAL), ({"scale": 0.0}, EINVAL), ({"scale": float("nan")}, EINVAL), ({"D": 96}, EUNSUPPORTED),
+                                       ({"K": 33, "Hq": 8}, EUNSUPPORTED), ({"K": 65, "Hq": 2}, EUNSUPPORTED), ({"C": 65536}, EUNSUPPORTED),
+                                       ({"max_pages": (1 << 24) + 1}, EUNSUPPORTED)])
+def test_scaled_draft_refuses_shapes(change, rc):
+    assert _draft_call(change) == rc
+    f = {"C_": 2, "K": 3, "Hq": 8, "Hkv": 2, "D": 64, "n_pages": 8, "max_pages": 40}
+    if "scale" not in change and "Hkv" not in change:
+        shape = pe.DecodeShape(**(f | {("C_" if n == "C" else n): x for n, x in change.items()}))
+        with pytest.raises(pe.PeagleError):
+            pe.peagle_draft_decode_scaled_workspace_bytes(shape)
+        assert pe.peagle_draft_decode_scaled_splits(shape) == -1
+
+
+def test_scaled_draft_refuses_formats_pointers_and_workspaces():
+    assert _draft_call(format_=2) == EUNSUPPORTED and _draft_call(format_=-1) == EUNSUPPORTED
+    for n in ("q_new", "k_new", "v_new", "k_pages", "v_pages", "k_scale", "v_scale", "block_table", "ctx_len", "o", "lse"):
+        assert _draft_call(**{n: None}) == ENULL, n
+    for n in ("q_new", "k_new", "v_new", "k_pages", "v_pages", "o"):
+        assert _draft_call(**{n: C.c_void_p(264)}) == EINVAL, n
+    assert _draft_call(workspace=None) == EWORKSPACE and _draft_call(ws_bytes=16) == EWORKSPACE
