@@ -478,7 +478,6 @@ int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, const void* k_
  * and values are bf16, as there.  Codes and scales become bf16 without rounding; scores, row sums and outputs are summed in
  * fp32, probabilities are rounded to bf16 before they weigh the values.
  */
-int32_t peagle_draft_decode_scaled_splits(const peagle_decode_shape_t* shape);
 size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode_shape_t* shape);
 int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,
                                const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale,

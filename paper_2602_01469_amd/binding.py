@@ -56,7 +56,7 @@ EXPORTS = [
     "peagle_draft_decode_splits", "peagle_draft_decode_workspace_bytes", "peagle_draft_decode",
     "peagle_draft_decode_static",
     "peagle_cache_plan_workspace_bytes", "peagle_cache_plan", "peagle_cache_append_scaled",
-    "peagle_draft_decode_scaled_splits", "peagle_draft_decode_scaled_workspace_bytes", "peagle_draft_decode_scaled",
+    "peagle_draft_decode_scaled_workspace_bytes", "peagle_draft_decode_scaled",
     "peagle_attn_step_profiled", "peagle_measure_mfma_ceiling", "peagle_measure_mfma_ceiling_random", "peagle_device_info", "peagle_strerror",
 ]
 
@@ -150,8 +150,6 @@ def load_library():
     lib.peagle_cache_plan.restype = C.c_int
     lib.peagle_cache_append_scaled.argtypes = [C.POINTER(_CacheShapeC), vp, vp, vp, vp, vp, vp, vp, vp]
     lib.peagle_cache_append_scaled.restype = C.c_int
-    lib.peagle_draft_decode_scaled_splits.argtypes = [C.POINTER(_DecodeShapeC)]
-    lib.peagle_draft_decode_scaled_splits.restype = i32
     lib.peagle_draft_decode_scaled_workspace_bytes.argtypes = [C.POINTER(_DecodeShapeC)]
     lib.peagle_draft_decode_scaled_workspace_bytes.restype = sz
     lib.peagle_draft_decode_scaled.argtypes = [C.POINTER(_DecodeShapeC), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
@@ -692,10 +690,6 @@ def peagle_cache_append_scaled(shape: CacheShape, k_new, v_new, slots, k_pages, 
     rc = load_library().peagle_cache_append_scaled(C.byref(c), k, v, at, *pools, _stream_ptr(stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_cache_append_scaled")
-
-
-def peagle_draft_decode_scaled_splits(shape: DecodeShape) -> int:
-    return int(load_library().peagle_draft_decode_scaled_splits(shape.c()))
 
 
 def peagle_draft_decode_scaled_workspace_bytes(shape: DecodeShape) -> int:

@@ -765,25 +765,27 @@ extern "C" int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, con
                                                                                                               : PEAGLE_EHIP;
 }
 
-// The drafting step on a cache held in 8 bits: partial records as above, for the pieces that the launch takes.
+// The drafting step on a cache held in 8 bits: two partial records for each workgroup that shares the work of a KV head.
 namespace {
 
-DecodeWs decode_scaled_ws(const peagle_decode_shape_t* s) {
-  DecodeWs w;
-  w.n_splits = peagle::draft_scaled_pieces((int64_t)s->C * s->Hkv, s->max_pages, s->D);
-  w.rows_pad = (s->K * (s->Hq / s->Hkv) + 31) / 32 * 32;
-  const size_t recs = w.n_splits > 1 ? (size_t)s->C * s->Hkv * w.n_splits : 0;
-  w.o_off = 0;
-  w.ml_off = align256(recs * w.rows_pad * s->D * sizeof(float));
-  w.total = w.ml_off + align256(recs * 3 * w.rows_pad * sizeof(float)) + 256;  // (never 0, which means a shape that is refused)
+struct ScaledWs {
+  DecodeWs records;  // n_splits: workgroups a KV head
+  size_t pieces_off, total;
+};
+ScaledWs decode_scaled_ws(const peagle_decode_shape_t* s) {
+  ScaledWs w;
+  DecodeWs& r = w.records;
+  r.n_splits = peagle::draft_scaled_shares(s->C, s->Hkv, s->max_pages);
+  r.rows_pad = (s->K * (s->Hq / s->Hkv) + 31) / 32 * 32;
+  const size_t recs = (size_t)s->Hkv * r.n_splits * 2;
+  r.o_off = 0;
+  r.ml_off = align256(recs * r.rows_pad * s->D * sizeof(float));
+  r.total = w.pieces_off = r.ml_off + align256(recs * 3 * r.rows_pad * sizeof(float));
+  w.total = w.pieces_off + align256((size_t)s->C * sizeof(int2));
   return w;
 }
 
 }  // namespace
-
-extern "C" int32_t peagle_draft_decode_scaled_splits(const peagle_decode_shape_t* shape) {
-  return check_decode(shape) == PEAGLE_OK ? decode_scaled_ws(shape).n_splits : -1;
-}
 
 extern "C" size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode_shape_t* shape) {
   return check_decode(shape) == PEAGLE_OK ? decode_scaled_ws(shape).total : 0;
@@ -800,10 +802,12 @@ extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, in
     return PEAGLE_ENULL;
   if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o))
     return PEAGLE_EINVAL;
-  const DecodeWs w = decode_scaled_ws(shape);
+  const ScaledWs w = decode_scaled_ws(shape);
   if (!workspace || ws_bytes < w.total) return PEAGLE_EWORKSPACE;
   peagle::ScaledDecodeParams p{};
-  p.d = decode_params(shape, w, q_new, k_new, v_new, block_table, ctx_len, o, lse, status, workspace);
+  p.shares = w.records.n_splits;
+  p.pieces = (int2*)((char*)workspace + w.pieces_off);
+  p.d = decode_params(shape, w.records, q_new, k_new, v_new, block_table, ctx_len, o, lse, status, workspace);
   p.k_pages = (const uint8_t*)k_pages;
   p.v_pages = (const uint8_t*)v_pages;
   p.k_scale = (const uint8_t*)k_scale;

@@ -114,22 +114,24 @@ struct DecodeParams {
   float c_log2;
 };
 hipError_t launch_draft_decode(const DecodeParams& p, int D, hipStream_t stream);
-// The merge of a drafting step's pieces; everything that its main kernel was given, more than one piece.
-hipError_t launch_draft_combine(const DecodeParams& p, int D, hipStream_t stream);
 // Pieces per request that the launch takes (host only): workgroups per piece are requests x KV heads, `laid_out` is the
 // number of pieces that the workspace has records for.
 int draft_pieces(int64_t wgs_per_piece, int max_pages, int laid_out, int D);
 
 // The drafting step on a cache that is held in 8 bits.
 struct ScaledDecodeParams {
-  DecodeParams d;          // k_pages, v_pages unused; n_splits, rows_pad as laid out
+  DecodeParams d;          // k_pages, v_pages, n_splits unused
   const uint8_t* k_pages;  // [n_pages, Hkv, 64, D]
   const uint8_t* v_pages;
   const uint8_t* k_scale;  // [n_pages, Hkv] codes of powers of two
   const uint8_t* v_scale;
+  int shares;              // workgroups that share the work of a KV head (0: one for each request); d.part_o, d.part_ml:
+                           // [Hkv, shares, 2] records
+  int2* pieces;            // workspace [C]: first of a request's records, number of them
+  int least_share;         // filled by the launcher: units a workgroup takes at least
 };
 hipError_t launch_draft_scaled(const ScaledDecodeParams& p, int D, bool e5m2, hipStream_t stream);
-int draft_scaled_pieces(int64_t wgs_per_piece, int max_pages, int D);
+int draft_scaled_shares(int C, int Hkv, int max_pages);
 
 // Optional per-kernel timing: an event pair is recorded around every launch on the launch stream.
 enum KernelKind { kKindFwd = 0, kKindDq = 1, kKindDkDv = 2, kKindReduce = 3, kKindRope = 4, kNumKinds = 5 };

@@ -3072,10 +3072,7 @@ hipError_t launch_draft_decode(const DecodeParams& pin, int D, hipStream_t strea
   };
   p.n_splits == 1 ? go(std::true_type{}) : go(std::false_type{});
   hipError_t e = hipGetLastError();
-  return e != hipSuccess || p.n_splits == 1 ? e : launch_draft_combine(p, D, stream);
-}
-
-hipError_t launch_draft_combine(const DecodeParams& p, int D, hipStream_t stream) {
+  if (e != hipSuccess || p.n_splits == 1) return e;
   // threads per row and splits per thread: n_splits is at most 32
   auto merge = [&](auto kernel, int rows_per_wave) {
     const int per_block = 4 * rows_per_wave;

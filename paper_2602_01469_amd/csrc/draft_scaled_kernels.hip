@@ -8,6 +8,7 @@
 #include "attn_kernels.h"
 #include "attn_util.h"
 
+#include <climits>
 #include <type_traits>
 
 namespace peagle {
@@ -123,125 +124,161 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* slot, co
   }
 }
 
-// The request's K new keys (bf16), straight from memory; the row of depth d sees keys 0..d.  k_new, v_new: key 0 of the KV head,
-// the next one `stride` elements on.  A masked key weighs zero, and zero times an infinity or NaN is NaN: such values are taken
-// out of the product and added to the rows that see them.
+// A block of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
+// the first of them key k0; the row of depth d sees keys 0..d.  A masked key weighs zero, and zero times an infinity or NaN is
+// NaN: such values are taken out of the product and added to the rows that see them, from v_new (key 0 of the KV head, the next
+// one `stride` elements on).
 template <int D, int RB>
-__device__ __forceinline__ void new_keys(Rows<D, RB>& r, const __bf16* k_new, const __bf16* v_new, uint32_t stride, int K,
+__device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* slot, int k0, int K, const __bf16* v_new, uint32_t stride,
                                          const int (&depth)[RB], float c) {
-  const int lane = lane_id(), g = lane >> 5, ln = lane & 31;
-  for (int k0 = 0; k0 < K; k0 += 32) {
-    const uint32_t row = (uint32_t)(k0 + ln < K ? k0 + ln : K - 1) * stride + 16 * g;
-    bf16x8 pb[RB][2];
-    f32x16 s[RB];
+  constexpr int kKeys = 2048 / D;  // of a slot
+  const int lane = lane_id(), g = lane >> 5, ln = lane & 31, row = ln % kKeys;
+  f32x16 s[RB];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
+  for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      const bf16x8 a = as_frag(ld16(k_new + row + ((i / 2) * 32 + (i % 2) * 8)));
+  for (int i = 0; i < D / 16; ++i) {
+    const bf16x8 a = *reinterpret_cast<const bf16x8*>(slot + tile_off<D>(row, 4 * (i / 2) + 2 * g + i % 2));
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) s[rb] = mfma32(a, r.q[rb][i], s[rb]);
+    for (int rb = 0; rb < RB; ++rb) s[rb] = mfma32(a, r.q[rb][i], s[rb]);
+  }
+  bf16x8 pb[RB][2];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int sees = depth[rb] + 1 - k0, n = sees < kKeys ? sees : kKeys;
+    const uint32_t bits = (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1) >> (4 * g);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
+    soft(r, rb, s[rb], c, pb[rb]);
+  }
+  bool odd = false;
+  const TrOff<D> to = tr_offsets<D>(lane);
+#pragma unroll
+  for (int t = 0; t < kKeys / 16; ++t)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      u32x4 a = __builtin_bit_cast(u32x4, frag_tr<D>(slot + 4096, to, t * 16, db));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w = a[j];
+        const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+        odd |= lo | hi;
+        a[j] = w & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(__builtin_bit_cast(bf16x8, a), pb[rb][t], r.o[rb][db]);
     }
+  if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+    for (int e = k0; e < K && e < k0 + kKeys; ++e) {
+      const uint32_t v = (uint32_t)e * stride + 4 * g;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int n = depth[rb] + 1 - k0;
-      const uint32_t bits = (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1) >> (4 * g);
+      for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
-      soft(r, rb, s[rb], c, pb[rb]);
-    }
-    bool odd = false;
+        for (int i4 = 0; i4 < 4; ++i4) {
+          __builtin_amdgcn_sched_barrier(0);  // (seldom here: few registers rather than many loads on their way)
+          const u32x2 w = *reinterpret_cast<const u32x2*>(v_new + v + (db * 32 + 8 * i4));
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (k0 + 16 * t >= K) break;
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t x = j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16;
+            const float add = (x & 0x7f800000u) == 0x7f800000u ? __builtin_bit_cast(float, x) : 0.f;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        u32x4 a;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          uint32_t pair = 0;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int at = k0 + 16 * t + 4 * g + (j < 4 ? 0 : 4) + j + h;
-            const uint32_t from = (uint32_t)(at < K ? at : K - 1) * stride + ln;
-            const uint32_t x = *reinterpret_cast<const uint16_t*>(v_new + from + db * 32);
-            const bool fine = (x & 0x7f80u) != 0x7f80u;
-            odd |= !fine;
-            pair |= (fine ? x : 0u) << (16 * h);
+            for (int rb = 0; rb < RB; ++rb) r.o[rb][db][4 * i4 + j] += depth[rb] >= e ? add : 0.f;
           }
-          a[j / 2] = pair;
         }
-        const bf16x8 frag = __builtin_bit_cast(bf16x8, a);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(frag, pb[rb][t], r.o[rb][db]);
-      }
-    }
-    if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-      for (int e = k0; e < K && e < k0 + 32; ++e) {
-        const uint32_t v = (uint32_t)e * stride + 4 * g;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4) {
-            __builtin_amdgcn_sched_barrier(0);  // (seldom here: few registers rather than many loads on their way)
-            const u32x2 w = *reinterpret_cast<const u32x2*>(v_new + v + (db * 32 + 8 * i4));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t x = j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16;
-              const float add = (x & 0x7f800000u) == 0x7f800000u ? __builtin_bit_cast(float, x) : 0.f;
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb) r.o[rb][db][4 * i4 + j] += depth[rb] >= e ? add : 0.f;
-            }
-          }
-      }
     }
   }
 }
 
-// Workgroup = (piece of a context, KV head, request), four waves.  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that
-// share the KV head (row = depth * group + head) and takes every n-th page of the piece by itself: it copies pages to a ring of
-// its own in LDS, two slots, and computes on one while the other is on its way, so that the loop has no barrier and a wave waits
-// for its own copies only.  The four waves hold the same rows (one block at D = 128, where two leave too few registers, one or two
-// at D = 64); more rows are shared out over two or all of them.  At the end the sums of waves with the same rows are merged
-// through LDS.  Eight waves a CU (two workgroups) have up to 128 KiB on their way.
-template <int D, bool E5M2, int RB>
+// Sum of x over the lanes up to and including this one.
+__device__ __forceinline__ int scan_lanes(int x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    x += lane >= d ? y : 0;
+  }
+  return x;
+}
+
+// Cached tokens of a request, clamped to what its table can describe.
+__device__ __forceinline__ int clamp_len(int n, int max_pages) {
+  return n < 0 ? 0 : n > max_pages * kKeysPerTile ? max_pages * kKeysPerTile : n;
+}
+__device__ __forceinline__ int pages_of(int n) { return (n + kKeysPerTile - 1) / kKeysPerTile; }
+
+// Every workgroup of a KV head takes the same share of all requests' work, counted in pages with one more for a request's new
+// keys: workgroup w the units [w share, (w + 1) share) of the requests one after the other.
+struct Share {
+  int share, c, skip;  // units a workgroup; its first request, and the units of that which others take
+  bool any;
+};
+__device__ __forceinline__ Share share_of(const int32_t* ctx_len, int C, int max_pages, int w, int n_wgs, int least, int lane) {
+  const int per = (C + 63) / 64;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int c = lane * per + i;
+    mine += c < C ? pages_of(clamp_len(ctx_len[c], max_pages)) + 1 : 0;
+  }
+  int end = scan_lanes(mine, lane);
+  const int total = __builtin_amdgcn_readlane(end, 63);
+  Share s;
+  s.share = (total + n_wgs - 1) / n_wgs;
+  s.share = s.share < least ? least : s.share;
+  const int64_t at64 = (int64_t)w * s.share;
+  s.any = at64 < total;
+  const int at = s.any ? (int)at64 : 0;
+  int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(end > at));
+  int before = __builtin_amdgcn_readlane(end - mine, l);
+  s.c = l * per;
+  if (per > 1) {
+    const int c = s.c + lane;
+    mine = lane < per && c < C ? pages_of(clamp_len(ctx_len[c], max_pages)) + 1 : 0;
+    end = before + scan_lanes(mine, lane);
+    l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(end > at));
+    before = __builtin_amdgcn_readlane(end - mine, l);
+    s.c += l;
+  }
+  s.skip = at - before;
+  return s;
+}
+
+template <int N, int PER>
+__device__ __forceinline__ void wait_slots(int pending) {  // until at most `pending` (<= N) slots' copies are on their way
+  if constexpr (N == 0) {
+    wait_outstanding<0>();
+  } else {
+    if (pending >= N) wait_outstanding<N * PER>();
+    else wait_slots<N - 1, PER>(pending);
+  }
+}
+
+// Workgroup = (share of the work, KV head), four waves.  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that share the
+// KV head (row = depth * group + head); PARTS waves with different rows make a stream, and the streams take a request's pages in
+// turn.  A stream has a ring of slots in LDS, filled by its waves some slots ahead of their use.  With one wave a stream (up to 32
+// rows, at D = 64 up to 64) a wave waits for its own copies only and the loop has no barrier; more rows share what a stream copies,
+// which costs a barrier a slot.  At the end of a request's pages the streams' sums are merged through LDS, and leave the results
+// where the request is one workgroup's, otherwise a partial record.
+template <int D, bool E5M2, int RB, int PARTS>
 __global__ __launch_bounds__(kWaves * 64, 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
   constexpr int kSubKeys = 4096 / D, kSubs = kKeysPerTile / kSubKeys;  // keys of a slot; slots of a page
+  constexpr int kNewKeys = 2048 / D;                                   // new keys of a slot
+  constexpr int kStreams = kWaves / PARTS, kDepth = 2 * PARTS, kPer = 8 / PARTS;  // slots of a ring; copies a wave issues for one
+  constexpr int kAhead = PARTS == 1 ? kDepth : kDepth - 1;             // slots on their way or in use
   const DecodeParams& p = sp.d;
-  __shared__ __attribute__((aligned(16))) char ring[kWaves][2][kSlotBytes];
+  __shared__ __attribute__((aligned(16))) char ring[kStreams][kDepth][kSlotBytes];
   __shared__ float stats[kWaves][RB * 32][2];  // of each wave's rows: reference, sum
   __shared__ int wave_bad[kWaves];
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 5, ln = lane & 31;
-  const int split = blockIdx.x, kvh = blockIdx.y, c = blockIdx.z;
-  const int share = p.rows_pad > 64 * RB ? 2 : p.rows_pad > 32 * RB ? 1 : 0;  // log2 of the waves that share the rows out
-  const int part = wave & ((1 << share) - 1), stream = wave >> share, n_streams = kWaves >> share;
+  const int kvh = blockIdx.y, part = wave % PARTS, stream = wave / PARTS;
   const int n_rows = p.K * p.group;
 
-  int n_ctx = p.ctx_len[c];
-  bool bad = n_ctx < 0 || n_ctx > p.max_pages * kKeysPerTile;
-  n_ctx = n_ctx < 0 ? 0 : (n_ctx > p.max_pages * kKeysPerTile ? p.max_pages * kKeysPerTile : n_ctx);
-  const int n_pg = (n_ctx + kKeysPerTile - 1) / kKeysPerTile;
-  int up = n_pg + p.n_splits - 1;
-  const int per = split_by(up, p.by_splits);
-  const int p0 = split * per < n_pg ? split * per : n_pg;
-  const int p1 = p0 + per < n_pg ? p0 + per : n_pg;
-  const int n_mine = p1 - p0 > stream ? (p1 - p0 - stream + n_streams - 1) / n_streams : 0;  // pages of this wave
-
-  Rows<D, RB> r;
-  int depth[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = (part * RB + rb) * 32 + ln;
-    depth[rb] = row < n_rows ? small_quotient(row, p.group_reciprocal) : 0;
-    const int head = kvh * p.group + (row < n_rows ? row - depth[rb] * p.group : 0);
-    const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 16 * g;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + (i / 2) * 32 + (i % 2) * 8));
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) r.o[rb][db] = zero16();
-    r.m[rb] = -3.402823466e38f;  // (any score is above it, and it less any score is no NaN)
-    r.l[rb] = 0.f;
+  int c = blockIdx.x, skip = 0, left = INT_MAX, share = 0;
+  if (sp.shares > 0) {
+    const Share s = share_of(p.ctx_len, p.C, p.max_pages, blockIdx.x, sp.shares, sp.least_share, lane);
+    if (!s.any) return;
+    c = s.c;
+    skip = s.skip;
+    left = share = s.share;
   }
 
   int k_off[D / 32], v_off[D / 32];
@@ -259,159 +296,332 @@ __global__ __launch_bounds__(kWaves * 64, 2) void draft_scaled_kernel(ScaledDeco
 #pragma unroll
   for (int b = 0; b < 2; ++b)
     voff[b] = (uint32_t)((lane / kLanes) * D + ((lane % kLanes ^ swz8<D>(b * (64 / kLanes) + lane / kLanes)) << 4));
-  const uint32_t ring_at = lds_scalar_addr(&ring[wave][0][0]);
-
-  for (int first = 0; first == 0 || first < n_mine; first += 64) {
-    // This wave's next pages, one a lane: page, keys present (0: page id outside the pool), scales.
-    const int pi = p0 + stream + n_streams * (first + lane);
-    const bool there = pi < p1;
-    int page = there ? p.block_table[(size_t)c * p.max_pages + pi] : 0;
-    const bool fine = page >= 0 && page < p.n_pages;
-    bad |= !fine;
-    page = fine ? page : 0;
-    const int keys_here = n_ctx - pi * kKeysPerTile;
-    int keys = !there || !fine ? 0 : keys_here < kKeysPerTile ? keys_here : kKeysPerTile;
-    int kcode = 0, vcode = 0;
-    if (there) {
-      kcode = sp.k_scale[(size_t)page * p.Hkv + kvh];
-      vcode = sp.v_scale[(size_t)page * p.Hkv + kvh];
+  const uint32_t ring_at = lds_scalar_addr(&ring[stream][0][0]);
+  // This wave's copies of a slot: f(which half, block of 1 KiB).
+  auto each_copy = [&](auto f) {
+    if constexpr (PARTS == 1) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) f(false, b);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) f(true, b);
+    } else {
+      const int b0 = part % (PARTS / 2) * kPer;
+#pragma unroll
+      for (int b = 0; b < kPer; ++b) f(part >= PARTS / 2, b0 + b);
     }
-    const int n_here = n_mine - first < 64 ? n_mine - first : 64;
-    const int n_sub = n_here > 0 ? n_here * kSubs : 0;
+  };
 
-    auto copy = [&](int s) {
-      const int j = s / kSubs, sub = s % kSubs;
-      const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (kKeysPerTile * D) + sub * 4096;
-      const uint8_t* kp = uniform_ptr(sp.k_pages + at);
-      const uint8_t* vp = uniform_ptr(sp.v_pages + at);
-      const uint32_t dst = ring_at + (uint32_t)(s & 1) * kSlotBytes;
-      const int present = __builtin_amdgcn_readlane(keys, j) - sub * kSubKeys;
-      if (present >= kSubKeys) {
+  for (int segment = 0;; ++segment) {
+    int n_ctx = p.ctx_len[c];
+    bool bad = n_ctx < 0 || n_ctx > p.max_pages * kKeysPerTile;
+    n_ctx = clamp_len(n_ctx, p.max_pages);
+    const int n_pg = pages_of(n_ctx), units = n_pg + 1;
+    const int n_units = units - skip < left ? units - skip : left;
+    const int p0 = skip, p1 = skip + n_units < n_pg ? skip + n_units : n_pg;
+    const bool has_new = skip + n_units == units, whole = n_units == units;
+
+    Rows<D, RB> r;
+    int depth[RB];
+    const int lane_here = lane_id();
 #pragma unroll
-        for (int b = 0; b < 4; ++b) dma16_untracked(kp + b * 1024, voff[b & 1], dst + b * 1024);
+    for (int rb = 0; rb < RB; ++rb) {
+      const int row = (part * RB + rb) * 32 + (lane_here & 31);
+      depth[rb] = row < n_rows ? small_quotient(row, p.group_reciprocal) : 0;
+      const int head = kvh * p.group + (row < n_rows ? row - depth[rb] * p.group : 0);
+      const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 16 * (lane_here >> 5);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) dma16_untracked(vp + b * 1024, voff[b & 1], dst + 4096 + b * 1024);
-      } else {  // rows behind the last token are read as that token: they are masked, and zero times its values adds nothing
-        const int last = present > 0 ? present - 1 : 0, l = lane_id();
+      for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + (i / 2) * 32 + (i % 2) * 8));
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int row = b * (64 / kLanes) + l / kLanes;
-          const uint32_t off = (uint32_t)((row < last ? row : last) * D + ((l % kLanes ^ swz8<D>(row)) << 4));
-          dma16_untracked(kp, off, dst + b * 1024);
-          dma16_untracked(vp, off, dst + 4096 + b * 1024);
-        }
+      for (int db = 0; db < D / 32; ++db) r.o[rb][db] = zero16();
+      r.m[rb] = -3.402823466e38f;  // (any score is above it, and it less any score is no NaN)
+      r.l[rb] = 0.f;
+    }
+
+    // The last stream's slots hold the new keys first.
+    const int n_new = has_new ? (p.K + kNewKeys - 1) / kNewKeys : 0, my_new = stream == kStreams - 1 ? n_new : 0;
+    const size_t new_at = ((size_t)c * p.K * p.Hkv + kvh) * D;
+    const __bf16* k_new = uniform_ptr(p.k_new + new_at);
+    const __bf16* v_new = uniform_ptr(p.v_new + new_at);
+    const int n_pages_0 = (p1 - p0 + kStreams - 1) / kStreams;  // pages of stream 0, the most
+    const int n_mine = p1 - p0 > stream ? (p1 - p0 - stream + kStreams - 1) / kStreams : 0;
+
+    for (int first = 0; first == 0 || first < n_pages_0; first += 64) {
+      // This stream's next pages, one a lane: page, keys present (0: page id outside the pool), scales.
+      const int pi = p0 + stream + kStreams * (first + lane_id());
+      const bool there = pi < p1;
+      int page = there ? p.block_table[(size_t)c * p.max_pages + pi] : 0;
+      const bool fine = page >= 0 && page < p.n_pages;
+      bad |= !fine;
+      page = fine ? page : 0;
+      const int keys_here = n_ctx - pi * kKeysPerTile;
+      const int keys = !there || !fine ? 0 : keys_here < kKeysPerTile ? keys_here : kKeysPerTile;
+      int kcode = 0, vcode = 0;
+      if (there) {
+        kcode = sp.k_scale[(size_t)page * p.Hkv + kvh];
+        vcode = sp.v_scale[(size_t)page * p.Hkv + kvh];
       }
-    };
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // (after 64 pages: the slots' last reads have left them)
-    if (n_sub > 0) copy(0);
-    if (n_sub > 1) copy(1);
-    if (first == 0 && split == 0 && stream == (p1 - p0) % n_streams) {
-      const size_t at = ((size_t)c * p.K * p.Hkv + kvh) * D;
-      new_keys<D, RB>(r, uniform_ptr(p.k_new + at), uniform_ptr(p.v_new + at), (uint32_t)(p.Hkv * D), p.K, depth, p.c_log2);
-    }
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own loads: none is waited for in the loop, behind its copies)
-    for (int s = 0; s < n_sub; ++s) {
-      if (s + 1 < n_sub) wait_outstanding<8>();
-      else wait_outstanding<0>();
-      const int j = s / kSubs, visible = __builtin_amdgcn_readlane(keys, j) - s % kSubs * kSubKeys;
-      const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
-      const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(vcode, j) << 23);
-      cached_keys<D, E5M2, RB>(r, ring[wave][s & 1], k_off, v_off, ks, vs, visible, g, p.c_log2);
-      if (s + 2 < n_sub) {
+      const int n_here = n_mine - first < 64 ? n_mine - first : 64;
+      const int q0 = first == 0 ? my_new : 0, n_q = q0 + (n_here > 0 ? n_here * kSubs : 0);  // slots: new keys', all
+
+      auto copy = [&](int q) {
+        const uint32_t dst = ring_at + (uint32_t)(q % kDepth) * kSlotBytes;
+        if (q < q0) {
+          const int l = lane_id();
+          each_copy([&](bool half, int b) {
+            const int row = b * (512 / D) + l / (D / 8), key = q * kNewKeys + row;
+            const uint32_t off = (uint32_t)(key < p.K ? key : p.K - 1) * (uint32_t)(p.Hkv * D * 2) + ((l % (D / 8) ^ swz<D>(row)) << 4);
+            dma16_untracked(half ? v_new : k_new, off, dst + (half ? 4096 : 0) + b * 1024);
+          });
+          return;
+        }
+        const int j = (q - q0) / kSubs, sub = (q - q0) % kSubs;
+        const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (kKeysPerTile * D) + sub * 4096;
+        const int present = __builtin_amdgcn_readlane(keys, j) - sub * kSubKeys;
+        if (present >= kSubKeys) {
+          each_copy([&](bool half, int b) {
+            dma16_untracked(uniform_ptr((half ? sp.v_pages : sp.k_pages) + at) + b * 1024, voff[b & 1], dst + (half ? 4096 : 0) + b * 1024);
+          });
+        } else {  // rows behind the last token are read as that token: they are masked, and zero times its values adds nothing
+          const int last = present > 0 ? present - 1 : 0, l = lane_id();
+          each_copy([&](bool half, int b) {
+            const int row = b * (64 / kLanes) + l / kLanes;
+            const uint32_t off = (uint32_t)((row < last ? row : last) * D + ((l % kLanes ^ swz8<D>(row)) << 4));
+            dma16_untracked(uniform_ptr((half ? sp.v_pages : sp.k_pages) + at), off, dst + (half ? 4096 : 0) + b * 1024);
+          });
+        }
+      };
+      int issued = 0;
+      for (; issued < kAhead && issued < n_q; ++issued) copy(issued);
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own loads: none is waited for in the loop, behind its copies)
+      // A slot's turn: what it holds has landed; with several waves a stream, everyone is done with the slot before it, which is
+      // filled again.
+      auto begin = [&](int q) {
+        if (q < n_q) wait_slots<kAhead - 1, kPer>(issued - 1 - q);
+        if (PARTS > 1) {
+          __syncthreads();
+          if (issued < n_q) copy(issued++);
+        }
+      };
+      auto end = [&] {
+        if (PARTS > 1) return;
         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot's last reads have left it
-        copy(s + 2);
+        if (issued < n_q) copy(issued++);
+      };
+      int q = 0;
+      if (first == 0) {
+        // (where streams meet at barriers, the others wait for the new keys' turns)
+        for (int i = 0; i < (PARTS > 1 ? n_new : my_new); ++i) {
+          if (my_new == 0) {
+            if (PARTS > 1) __syncthreads();
+            continue;
+          }
+          begin(q);
+          new_keys<D, RB>(r, ring[stream][q % kDepth], q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+          end();
+          ++q;
+        }
       }
+      const int rounds = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) * kSubs : n_q - q0;
+      for (int i = 0; i < rounds; ++i, ++q) {
+        begin(q);
+        if (q < n_q) {
+          const int j = i / kSubs, visible = __builtin_amdgcn_readlane(keys, j) - i % kSubs * kSubKeys;
+          const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
+          const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(vcode, j) << 23);
+          cached_keys<D, E5M2, RB>(r, ring[stream][q % kDepth], k_off, v_off, ks, vs, visible, g, p.c_log2);
+        }
+        end();
+      }
+      if (PARTS > 1) __syncthreads();  // (the slots' last reads have left them)
     }
-  }
 
-  // Merge of the waves that hold the same rows: each leaves reference, sum and O (32 rows at a time, in its ring, 16 bytes of
-  // features by 16 bytes, the rows of feature group d4 in the order row ^ d4), and the threads add them up in order.
-  bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    // Merge of the waves that hold the same rows: each leaves reference, sum and O (32 rows at a time, in its part of the rings, 16
+    // bytes of features by 16 bytes, the rows of feature group d4 in the order row ^ d4), and the threads add them up in order.
+    bad = __builtin_amdgcn_ballot_w64(bad) != 0;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const float l = sum_halves(r.l[rb]);
-    if (g == 0) {
-      stats[wave][rb * 32 + ln][0] = r.m[rb];
-      stats[wave][rb * 32 + ln][1] = l;
-    }
-  }
-  if (lane == 0) wave_bad[wave] = bad;
-  f32x4* mine = reinterpret_cast<f32x4*>(&ring[wave][0][0]);
-  const int l = lane_id();
-  static_assert(32 * D * 4 <= 2 * kSlotBytes, "32 rows of O must fit a wave's ring");
-  const size_t rec = ((size_t)c * p.Hkv + kvh) * p.n_splits + split;
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    if (rb > 0) __syncthreads();
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const int d4 = db * 8 + 2 * i4 + (l >> 5);
-        mine[d4 * 32 + ((l ^ d4) & 31)] = f32x4{r.o[rb][db][4 * i4], r.o[rb][db][4 * i4 + 1], r.o[rb][db][4 * i4 + 2], r.o[rb][db][4 * i4 + 3]};
-      }
-    __syncthreads();
-    const bool any_bad = (wave_bad[0] | wave_bad[1] | wave_bad[2] | wave_bad[3]) != 0;
-    for (int item = wave * 64 + l; item < (32 << share) * (D / 4); item += kWaves * 64) {
-      const int d4 = item % (D / 4), in_block = item / (D / 4) % 32, h = item / (32 * (D / 4));
-      const int row = (h * RB + rb) * 32 + in_block;
-      float M = stats[h][rb * 32 + in_block][0];
-      for (int s = 1; s < n_streams; ++s) M = __builtin_fmaxf(M, stats[(s << share) + h][rb * 32 + in_block][0]);
-      float L = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < n_streams; ++s) {
-        const int w = (s << share) + h;
-        const float f = exp2_fast(stats[w][rb * 32 + in_block][0] - M);
-        L = __builtin_fmaf(stats[w][rb * 32 + in_block][1], f, L);
-        o += reinterpret_cast<const f32x4*>(&ring[w][0][0])[d4 * 32 + (in_block ^ (d4 & 31))] * f;
-      }
-      if (p.n_splits == 1) {
-        if (row < n_rows) {
-          const int dep = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - dep * p.group);
-          const float inv = 1.0f / L;
-          u32x2 out;
-          out[0] = pack_bf16(o[0] * inv, o[1] * inv);
-          out[1] = pack_bf16(o[2] * inv, o[3] * inv);
-          *reinterpret_cast<u32x2*>(p.o + (((size_t)c * p.K + dep) * p.Hq + head) * D + d4 * 4) = out;
-          if (d4 == 0) p.lse[((size_t)c * p.Hq + head) * p.K + dep] = (M + __builtin_log2f(L)) * kLn2;
-        }
-      } else if (row < p.rows_pad) {
-        *reinterpret_cast<f32x4*>(p.part_o + (rec * p.rows_pad + row) * D + d4 * 4) = o;
-        if (d4 == 0) {
-          float* ml = p.part_ml + rec * 3 * p.rows_pad + row;
-          ml[0] = M;
-          ml[p.rows_pad] = L;
-          ml[2 * p.rows_pad] = any_bad ? 1.f : 0.f;
-        }
+    for (int rb = 0; rb < RB; ++rb) {
+      const float l = sum_halves(r.l[rb]);
+      if (g == 0) {
+        stats[wave][rb * 32 + ln][0] = r.m[rb];
+        stats[wave][rb * 32 + ln][1] = l;
       }
     }
-    if (rb == 0 && p.n_splits == 1 && p.status && kvh == 0 && tid == 0) p.status[c] = any_bad;
+    if (lane == 0) wave_bad[wave] = bad;
+    constexpr int kRegion = 2 * kSlotBytes / 16;
+    static_assert(32 * D / 4 <= kRegion, "32 rows of O must fit a wave's part of the rings");
+    f32x4* regions = reinterpret_cast<f32x4*>(&ring[0][0][0]);
+    const int l = lane_id();
+    const size_t rec = ((size_t)kvh * gridDim.x + blockIdx.x) * 2 + (segment > 0 ? 1 : 0);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      if (rb > 0) __syncthreads();
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int d4 = db * 8 + 2 * i4 + (l >> 5);
+          regions[wave * kRegion + d4 * 32 + ((l ^ d4) & 31)] =
+              f32x4{r.o[rb][db][4 * i4], r.o[rb][db][4 * i4 + 1], r.o[rb][db][4 * i4 + 2], r.o[rb][db][4 * i4 + 3]};
+        }
+      __syncthreads();
+      const bool any_bad = (wave_bad[0] | wave_bad[1] | wave_bad[2] | wave_bad[3]) != 0;
+      for (int item = wave * 64 + l; item < 32 * PARTS * (D / 4); item += kWaves * 64) {
+        const int d4 = item % (D / 4), in_block = item / (D / 4) % 32, h = item / (32 * (D / 4));
+        const int row = (h * RB + rb) * 32 + in_block;
+        float M = stats[h][rb * 32 + in_block][0];
+#pragma unroll
+        for (int s = 1; s < kStreams; ++s) M = __builtin_fmaxf(M, stats[s * PARTS + h][rb * 32 + in_block][0]);
+        float L = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < kStreams; ++s) {
+          const int w = s * PARTS + h;
+          const float f = exp2_fast(stats[w][rb * 32 + in_block][0] - M);
+          L = __builtin_fmaf(stats[w][rb * 32 + in_block][1], f, L);
+          o += regions[w * kRegion + d4 * 32 + (in_block ^ (d4 & 31))] * f;
+        }
+        if (whole) {
+          if (row < n_rows) {
+            const int dep = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - dep * p.group);
+            const float inv = 1.0f / L;
+            u32x2 out;
+            out[0] = pack_bf16(o[0] * inv, o[1] * inv);
+            out[1] = pack_bf16(o[2] * inv, o[3] * inv);
+            *reinterpret_cast<u32x2*>(p.o + (((size_t)c * p.K + dep) * p.Hq + head) * D + d4 * 4) = out;
+            if (d4 == 0) p.lse[((size_t)c * p.Hq + head) * p.K + dep] = (M + __builtin_log2f(L)) * kLn2;
+          }
+        } else if (row < p.rows_pad) {
+          *reinterpret_cast<f32x4*>(p.part_o + (rec * p.rows_pad + row) * D + d4 * 4) = o;
+          if (d4 == 0) {
+            float* ml = p.part_ml + rec * 3 * p.rows_pad + row;
+            ml[0] = M;
+            ml[p.rows_pad] = L;
+            ml[2 * p.rows_pad] = any_bad ? 1.f : 0.f;
+          }
+        }
+      }
+      if (rb == 0 && tid == 0 && kvh == 0) {
+        if (whole && p.status) p.status[c] = any_bad;
+        // where the request's records stand: the first, and how many workgroups leave one
+        if (share > 0 && skip == 0) sp.pieces[c] = make_int2((int)blockIdx.x * 2 + (segment > 0 ? 1 : 0), 1 + (units - n_units + share - 1) / share);
+      }
+    }
+    left -= n_units;
+    skip = 0;
+    if (sp.shares == 0 || ++c >= p.C || left <= 0) return;
+    __syncthreads();  // the merge's reads have left the rings
   }
 }
 
+// Merges a request's partial records: M = max m_s, L = sum l_s 2^(m_s - M), O = sum O_s 2^(m_s - M) / L.  kLanes threads per (row,
+// 4 features) take the records in turn, kEach at a time, whose loads are issued before the first is used.
+template <int D>
+__global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeParams sp) {
+  constexpr int kLanes = 256 / D, kEach = 4;
+  const DecodeParams& p = sp.d;
+  const int lane = threadIdx.x & 63, d4 = lane % (D / 4), sl = lane / (D / 4);
+  const int kvh = blockIdx.y, c = blockIdx.z, n_rows = p.K * p.group;
+  const int2 piece = sp.pieces[c];
+  const int n = piece.y;
+  if (n <= 1) return;  // (its workgroup has left the results)
+  const int row = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
+  if (row >= n_rows) return;
+  // record 0 may be its workgroup's second, the others are their workgroups' first
+  const size_t rec0 = (size_t)kvh * sp.shares * 2;
+  auto record = [&](int s) { return rec0 + (s == 0 ? piece.x : (piece.x / 2 + s) * 2); };
+  float M = -3.402823466e38f, L = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  bool bad = false;
+  for (int s0 = 0; s0 < n; s0 += kLanes * kEach) {
+    float mv[kEach], lv[kEach], fv[kEach];
+    f32x4 ov[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {  // (records past the last are read as the last and weigh nothing)
+      const int s = s0 + j * kLanes + sl;
+      const size_t rec = record(s < n ? s : n - 1);
+      const float* ml = p.part_ml + rec * 3 * p.rows_pad + row;
+      mv[j] = ml[0];
+      lv[j] = ml[p.rows_pad];
+      fv[j] = ml[2 * p.rows_pad];
+      ov[j] = *reinterpret_cast<const f32x4*>(p.part_o + (rec * p.rows_pad + row) * D + d4 * 4);
+    }
+    float m_new = M;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) m_new = __builtin_fmaxf(m_new, mv[j]);
+    const float turn = exp2_fast(M - m_new);
+    M = m_new;
+    L *= turn;
+    acc *= turn;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const float w = s0 + j * kLanes + sl < n ? exp2_fast(mv[j] - M) : 0.f;
+      L = __builtin_fmaf(lv[j], w, L);
+      acc += ov[j] * w;
+      bad |= fv[j] != 0.f;
+    }
+  }
+#pragma unroll
+  for (int x = D / 4; x < 64; x <<= 1) {
+    const float m_other = __shfl_xor(M, x), l_other = __shfl_xor(L, x), m_new = __builtin_fmaxf(M, m_other);
+    const float a = exp2_fast(M - m_new), b = exp2_fast(m_other - m_new);
+    M = m_new;
+    L = L * a + l_other * b;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + __shfl_xor(acc[j], x) * b;
+  }
+  if (p.status && row == 0 && kvh == 0) {
+    const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
+    if (lane == 0) p.status[c] = any;
+  }
+  if (sl != 0) return;
+  const float inv = 1.0f / L;
+  const int depth = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - depth * p.group);
+  u32x2 out;
+  out[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
+  out[1] = pack_bf16(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<u32x2*>(p.o + (((size_t)c * p.K + depth) * p.Hq + head) * D + d4 * 4) = out;
+  if (d4 == 0) p.lse[((size_t)c * p.Hq + head) * p.K + depth] = (M + __builtin_log2f(L)) * kLn2;
+}
+
 constexpr int kCus = 256;  // compute units of the device
+constexpr int kLeastShare = 8;  // pages
 
 }  // namespace
 
-// Pieces of a request: two workgroups per CU in all where each wave still has a page of its own.
-int draft_scaled_pieces(int64_t wgs_per_piece, int max_pages, int) {
-  const int64_t want = (2 * kCus + wgs_per_piece - 1) / wgs_per_piece, most = (max_pages + kWaves - 1) / kWaves;
-  const int64_t n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : n > 32 ? 32 : n);
+// Workgroups that share the work of a KV head, 0: a workgroup for each request.
+int draft_scaled_shares(int C, int Hkv, int max_pages) {
+  if (C > 1024 || max_pages < kLeastShare || (int64_t)C * (max_pages + 1) > INT_MAX) return 0;
+  const int64_t slots = (2 * kCus + Hkv - 1) / Hkv, most = ((int64_t)C * (max_pages + 1) + kLeastShare - 1) / kLeastShare;
+  return (int)(slots < most ? slots : most);
 }
 
 hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, hipStream_t stream) {
   ScaledDecodeParams p = pin;
   p.d.group = p.d.Hq / p.d.Hkv;
   p.d.group_reciprocal = small_reciprocal(p.d.group);
-  p.d.by_splits = make_divisor(p.d.n_splits);
-  const dim3 grid((unsigned)p.d.n_splits, (unsigned)p.d.Hkv, (unsigned)p.d.C);
+  p.least_share = kLeastShare;
+  const dim3 grid((unsigned)(p.shares > 0 ? p.shares : p.d.C), (unsigned)p.d.Hkv);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), 0, stream, p); };
-  if (D == 128) e5m2 ? run(draft_scaled_kernel<128, true, 1>) : run(draft_scaled_kernel<128, false, 1>);
-  else if (p.d.rows_pad == 32) e5m2 ? run(draft_scaled_kernel<64, true, 1>) : run(draft_scaled_kernel<64, false, 1>);
-  else e5m2 ? run(draft_scaled_kernel<64, true, 2>) : run(draft_scaled_kernel<64, false, 2>);
+  auto go = [&](auto type) {
+    constexpr bool T = decltype(type)::value;
+    const int blocks = p.d.rows_pad / 32;
+    if (D == 64) {
+      if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1>);
+      else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1>);
+      else run(draft_scaled_kernel<64, T, 2, 2>);
+    } else {
+      if (blocks == 1) run(draft_scaled_kernel<128, T, 1, 1>);
+      else if (blocks == 2) run(draft_scaled_kernel<128, T, 1, 2>);
+      else run(draft_scaled_kernel<128, T, 1, 4>);
+    }
+  };
+  e5m2 ? go(std::true_type{}) : go(std::false_type{});
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || p.d.n_splits == 1 ? e : launch_draft_combine(p.d, D, stream);
+  if (e != hipSuccess || p.shares == 0) return e;
+  const dim3 rows((unsigned)((p.d.K * p.d.group + 3) / 4), (unsigned)p.d.Hkv, (unsigned)p.d.C);
+  if (D == 64) hipLaunchKernelGGL(draft_scaled_combine_kernel<64>, rows, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL(draft_scaled_combine_kernel<128>, rows, dim3(256), 0, stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace peagle

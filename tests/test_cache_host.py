@@ -157,7 +157,6 @@ def test_scaled_draft_refuses_shapes(change, rc):
         shape = pe.DecodeShape(**(f | {("C_" if n == "C" else n): x for n, x in change.items()}))
         with pytest.raises(pe.PeagleError):
             pe.peagle_draft_decode_scaled_workspace_bytes(shape)
-        assert pe.peagle_draft_decode_scaled_splits(shape) == -1
 
 
 def test_scaled_draft_refuses_formats_pointers_and_workspaces():

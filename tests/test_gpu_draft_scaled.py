@@ -267,7 +267,6 @@ def test_draft_scaled_replays_from_a_graph_and_runs_on_other_streams():
     same call on a stream of its own."""
     print("case scaled graph", flush=True)
     r = ScaledRun((1500, 70, 640), 5, 16, 2, 64, "e4m3", 3700)
-    assert pe.peagle_draft_decode_scaled_splits(r.shape) > 1
     r.run()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
