@@ -775,12 +775,12 @@ struct ScaledWs {
 ScaledWs decode_scaled_ws(const peagle_decode_shape_t* s) {
   ScaledWs w;
   DecodeWs& r = w.records;
-  r.n_splits = peagle::draft_scaled_shares(s->C, s->Hkv, s->max_pages);
   r.rows_pad = (s->K * (s->Hq / s->Hkv) + 31) / 32 * 32;
+  r.n_splits = peagle::draft_scaled_rule(s->C, s->Hkv, s->max_pages, r.rows_pad / 32, s->D).shares;
   const size_t recs = (size_t)s->Hkv * r.n_splits * 2;
   r.o_off = 0;
   r.ml_off = align256(recs * r.rows_pad * s->D * sizeof(float));
-  r.total = w.pieces_off = r.ml_off + align256(recs * 3 * r.rows_pad * sizeof(float));
+  r.total = w.pieces_off = r.ml_off + align256(recs * 4 * r.rows_pad * sizeof(float));
   w.total = w.pieces_off + align256((size_t)s->C * sizeof(int2));
   return w;
 }
@@ -805,7 +805,6 @@ extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, in
   const ScaledWs w = decode_scaled_ws(shape);
   if (!workspace || ws_bytes < w.total) return PEAGLE_EWORKSPACE;
   peagle::ScaledDecodeParams p{};
-  p.shares = w.records.n_splits;
   p.pieces = (int2*)((char*)workspace + w.pieces_off);
   p.d = decode_params(shape, w.records, q_new, k_new, v_new, block_table, ctx_len, o, lse, status, workspace);
   p.k_pages = (const uint8_t*)k_pages;

@@ -125,13 +125,17 @@ struct ScaledDecodeParams {
   const uint8_t* v_pages;
   const uint8_t* k_scale;  // [n_pages, Hkv] codes of powers of two
   const uint8_t* v_scale;
-  int shares;              // workgroups that share the work of a KV head (0: one for each request); d.part_o, d.part_ml:
-                           // [Hkv, shares, 2] records
   int2* pieces;            // workspace [C]: first of a request's records, number of them
-  int least_share;         // filled by the launcher: units a workgroup takes at least
+  int shares, least_share, lead;  // filled by the launcher, as in ShareRule; [Hkv, shares, 2]
+                           // records: d.part_o [rows_pad, D], d.part_ml [rows_pad, 4] reference, sums, flag
 };
 hipError_t launch_draft_scaled(const ScaledDecodeParams& p, int D, bool e5m2, hipStream_t stream);
-int draft_scaled_shares(int C, int Hkv, int max_pages);
+struct ShareRule {
+  int shares;  // workgroups that share the work of a KV head (0: one for each request)
+  int least;   // units that a workgroup takes at least
+  int lead;    // units that the start of a request counts for
+};
+ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D);  // blocks: of 32 query rows
 
 // Optional per-kernel timing: an event pair is recorded around every launch on the launch stream.
 enum KernelKind { kKindFwd = 0, kKindDq = 1, kKindDkDv = 2, kKindReduce = 3, kKindRope = 4, kNumKinds = 5 };

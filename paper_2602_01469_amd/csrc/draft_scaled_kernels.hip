@@ -1,12 +1,15 @@
 // The inference-side drafting step (Sec. 2 of the paper) on a paged cache that is held in 8 bits with a power-of-two scale for
 // each page and KV head: the K new rows of each request see its cached keys and the new keys of their own chain.
 //
-// With k = 2^ek a and v = 2^ev b for the codes a, b of a page, S = scale Q K^T, P = 2^(S log2(e) - m), O = P V / sum P.  The
-// type's values have four significant bits or three, so that a code times its page's scale is a bf16 number: codes are widened to
-// bf16 with the scale in one instruction for two of them, between LDS and the matrix instruction, exactly.
+// With k = 2^ek a and v = 2^ev b for the codes a, b of a page, S = scale Q K^T, P = 2^(S log2(e) - m), O = P V / sum P.  A code
+// has four significant bits or three, so that with its page's scale it is a bf16 number: codes are widened to bf16, scale and all, by
+// one instruction for two of them, between LDS and the matrix instruction.  (The matrix instruction for 8-bit types, with queries
+// split into two numbers of them, would need no widening of keys, but its sums are not fp32 sums: 64 products of normal data came
+// out 4e-5 of the largest sum off.)
 // The cache is read once, 2 Hkv D bytes a token, and bounds a large call; a small one is a chain of memory round trips.
 #include "attn_kernels.h"
 #include "attn_util.h"
+#include "cache_kernels.h"
 
 #include <climits>
 #include <type_traits>
@@ -14,8 +17,6 @@
 namespace peagle {
 
 namespace {
-
-constexpr int kWaves = 4, kSlotBytes = 8192;  // a slot of a wave's ring: 4 KiB of K, 4 KiB of V
 
 // Eight codes, times `scale` (a power of two), as a matrix operand.
 template <bool E5M2>
@@ -33,7 +34,7 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float scale) {
   return __builtin_bit_cast(bf16x8, u);
 }
 
-// LDS image of 4 KiB of a page, row (token) by row of D bytes: the 16-byte chunk c of row r stands at c ^ swz8(r), so that both
+// LDS image of 32 tokens of a page, row (token) by row of D bytes: the 16-byte chunk c of row r stands at c ^ swz8(r), so that both
 // reads below touch sixteen different 16-byte places modulo 256 bytes at a time:
 //   keys    lane <-> row, 16 rows, the same chunk
 //   values  rows {0..3, 8..11} or {4..7, 12..15} of a group of sixteen, two neighbouring chunks
@@ -50,126 +51,142 @@ template <int D, int RB>
 struct Rows {
   bf16x8 q[RB][D / 16];  // features 32 i + 16 g + 8 j .. + 8 of step 2 i + j
   f32x16 o[RB][D / 32];
-  float m[RB], l[RB];    // reference of the exponents (log2), sum over this lane's keys
+  float m[RB];           // reference of the exponents (log2)
+  float l[RB], w[RB];    // sums over this lane's keys of the probabilities: as they are, and as they weigh the values
 };
 
 // Scores of 32 keys (registers <-> keys 8 (i / 4) + 4 g + i % 4) to probabilities, as operands of the product with the values.
-// The reference is the running maximum.  The row sum takes the probabilities unrounded.
+// A probability is rounded to bf16 to weigh its value, by up to 2^-9 of itself wherever it stands, so that the reference need not be
+// near the row's largest score.  It must not be far below it: it moves where a lane's sum of probabilities says so (also at the first
+// keys, which meet the start value), and no maximum is taken otherwise.  The output is divided by the sum of the rounded
+// probabilities, which makes a row of one heavy key exact; the LSE takes the sum of the unrounded ones.
 template <int D, int RB>
-__device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, f32x16& s, float c, bf16x8 (&pb)[2]) {
-  const float mx = max_halves(max16(s)) * c;
-  const bool need = mx > r.m[rb];
-  if (__builtin_amdgcn_ballot_w64(need) != 0) {
+__device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, const f32x16& s, float c, bf16x8 (&pb)[2]) {
+  f32x16 x;
+  auto weigh = [&] {
+    float sum[4];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = exp2_fast(__builtin_fmaf(s[i], c, -r.m[rb]));
+      sum[i % 4] = i < 4 ? x[i] : sum[i % 4] + x[i];
+    }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  float sum = weigh();
+  if (__builtin_amdgcn_ballot_w64(sum > 0x1p40f) != 0) {
+    const float mx = max_halves(max16(s)) * c;
+    const bool need = max_halves(sum) > 0x1p40f && mx > r.m[rb];
     const float m_new = need ? mx : r.m[rb], alpha = exp2_fast(r.m[rb] - m_new);
     r.m[rb] = m_new;
     r.l[rb] *= alpha;
+    r.w[rb] *= alpha;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) r.o[rb][db][i] *= alpha;
+    sum = weigh();
   }
-  const float neg_m = -r.m[rb];
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    s[i] = exp2_fast(__builtin_fmaf(s[i], c, neg_m));
-    sum[i % 4] += s[i];
-  }
-  r.l[rb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  pb[0] = pack8(s, 0);
-  pb[1] = pack8(s, 1);
+  r.l[rb] += sum;
+  pb[0] = pack8_sum(x, 0, r.w[rb]);
+  pb[1] = pack8_sum(x, 1, r.w[rb]);
 }
 
-// Keys of a slot, `visible` of its first keys (the others are masked; their values are finite).
+// The 32 keys of a slot, of which the first n count (the others are masked; their values are finite).
 template <int D, bool E5M2, int RB>
 __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* slot, const int (&k_off)[D / 32], const int (&v_off)[D / 32],
-                                            float ks, float vs, int visible, int g, float c) {
+                                            float ks, float vs, int n, int g, float c) {
+  // All LDS reads first: one at a time in front of its use, as the compiler places them otherwise, each would be waited for.
+  typedef __attribute__((ext_vector_type(2))) int i32x2;
+  u32x4 kw[D / 32];
+  i32x2 vw[2][D / 32];
 #pragma unroll
-  for (int kb = 0; kb < 4096 / D / 32; ++kb) {
-    const int n = visible - kb * 32;
-    if (n <= 0) break;
-    bf16x8 pb[RB][2];
-    f32x16 s[RB];
+  for (int i = 0; i < D / 32; ++i) kw[i] = *reinterpret_cast<const u32x4*>(slot + k_off[i]);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(slot + k_off[i] + kb * 32 * D);
-      const bf16x8 a0 = widen8<E5M2>(w[0], w[1], ks), a1 = widen8<E5M2>(w[2], w[3], ks);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        s[rb] = mfma32(a0, r.q[rb][2 * i], s[rb]);
-        s[rb] = mfma32(a1, r.q[rb][2 * i + 1], s[rb]);
-      }
-    }
-    if (n < 32) {
-      const uint32_t bits = ((1u << n) - 1) >> (4 * g);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
-    }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) soft(r, rb, s[rb], c, pb[rb]);
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        typedef __attribute__((ext_vector_type(2))) int i32x2;
-        const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(PEAGLE_LDS_PTR(i32x2, slot + 4096 + v_off[db] + (kb * 2 + t) * 16 * D));
-        const bf16x8 a = widen8<E5M2>((uint32_t)w[0], (uint32_t)w[1], vs);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(a, pb[rb][t], r.o[rb][db]);
-      }
-  }
-}
-
-// A block of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
-// the first of them key k0; the row of depth d sees keys 0..d.  A masked key weighs zero, and zero times an infinity or NaN is
-// NaN: such values are taken out of the product and added to the rows that see them, from v_new (key 0 of the KV head, the next
-// one `stride` elements on).
-template <int D, int RB>
-__device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* slot, int k0, int K, const __bf16* v_new, uint32_t stride,
-                                         const int (&depth)[RB], float c) {
-  constexpr int kKeys = 2048 / D;  // of a slot
-  const int lane = lane_id(), g = lane >> 5, ln = lane & 31, row = ln % kKeys;
+    for (int db = 0; db < D / 32; ++db)
+      vw[t][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(PEAGLE_LDS_PTR(i32x2, slot + 32 * D + v_off[db] + t * 16 * D));
+  __builtin_amdgcn_sched_barrier(0);
   f32x16 s[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const bf16x8 a = *reinterpret_cast<const bf16x8*>(slot + tile_off<D>(row, 4 * (i / 2) + 2 * g + i % 2));
+  for (int i = 0; i < D / 32; ++i) {
+    const bf16x8 a0 = widen8<E5M2>(kw[i][0], kw[i][1], ks), a1 = widen8<E5M2>(kw[i][2], kw[i][3], ks);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb] = mfma32(a, r.q[rb][i], s[rb]);
+    for (int rb = 0; rb < RB; ++rb) {
+      s[rb] = mfma32(a0, r.q[rb][2 * i], s[rb]);
+      s[rb] = mfma32(a1, r.q[rb][2 * i + 1], s[rb]);
+    }
+  }
+  if (n < 32) {
+    const uint32_t bits = ((1u << n) - 1) >> (4 * g);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
   }
   bf16x8 pb[RB][2];
 #pragma unroll
+  for (int rb = 0; rb < RB; ++rb) soft(r, rb, s[rb], c, pb[rb]);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const bf16x8 a = widen8<E5M2>((uint32_t)vw[t][db][0], (uint32_t)vw[t][db][1], vs);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(a, pb[rb][t], r.o[rb][db]);
+    }
+}
+
+// Sixteen of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
+// the first of them key k0; the row of depth d sees keys 0..d.  A masked key weighs zero, and zero times an infinity or NaN is
+// NaN: such values are taken out of the product and added to the rows that see them, from v_new (key 0 of the KV head, the next
+// one `stride` elements on).
+constexpr int kNewKeys = 16;
+template <int D, int RB>
+__device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* slot, int k0, int K, const __bf16* v_new, uint32_t stride,
+                                         const int (&depth)[RB], float c) {
+  const int lane = lane_id(), g = lane >> 5, row = lane % kNewKeys;
+  bf16x8 ka[D / 16], va[D / 32];
+  const TrOff<D> to = tr_offsets<D>(lane);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(slot + tile_off<D>(row, 4 * (i / 2) + 2 * g + i % 2));
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) va[db] = frag_tr<D>(slot + 32 * D, to, 0, db);
+  __builtin_amdgcn_sched_barrier(0);
+  f32x16 s[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) s[rb] = mfma32(ka[i], r.q[rb][i], s[rb]);
+  bf16x8 pb[RB][2];
+#pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int sees = depth[rb] + 1 - k0, n = sees < kKeys ? sees : kKeys;
-    const uint32_t bits = (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1) >> (4 * g);
+    const int sees = depth[rb] + 1 - k0, n = sees < kNewKeys ? sees : kNewKeys;
+    const uint32_t bits = (n <= 0 ? 0u : (1u << n) - 1) >> (4 * g);
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
     soft(r, rb, s[rb], c, pb[rb]);
   }
   bool odd = false;
-  const TrOff<D> to = tr_offsets<D>(lane);
 #pragma unroll
-  for (int t = 0; t < kKeys / 16; ++t)
+  for (int db = 0; db < D / 32; ++db) {
+    u32x4 a = __builtin_bit_cast(u32x4, va[db]);
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      u32x4 a = __builtin_bit_cast(u32x4, frag_tr<D>(slot + 4096, to, t * 16, db));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w = a[j];
-        const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
-        odd |= lo | hi;
-        a[j] = w & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-      }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(__builtin_bit_cast(bf16x8, a), pb[rb][t], r.o[rb][db]);
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = a[j];
+      const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+      odd |= lo | hi;
+      a[j] = w & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
     }
-  if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-    for (int e = k0; e < K && e < k0 + kKeys; ++e) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(__builtin_bit_cast(bf16x8, a), pb[rb][0], r.o[rb][db]);
+  }
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
+    for (int e = k0; e < K && e < k0 + kNewKeys; ++e) {
       const uint32_t v = (uint32_t)e * stride + 4 * g;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
@@ -190,12 +207,13 @@ __device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* slot, int k
 }
 
 // Sum of x over the lanes up to and including this one.
-__device__ __forceinline__ int scan_lanes(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    x += lane >= d ? y : 0;
-  }
+__device__ __forceinline__ int scan_lanes(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // within rows of 16 lanes: from 1, 2, 4, 8 lanes below
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of rows 0 and 2 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
   return x;
 }
 
@@ -205,22 +223,27 @@ __device__ __forceinline__ int clamp_len(int n, int max_pages) {
 }
 __device__ __forceinline__ int pages_of(int n) { return (n + kKeysPerTile - 1) / kKeysPerTile; }
 
-// Every workgroup of a KV head takes the same share of all requests' work, counted in pages with one more for a request's new
-// keys: workgroup w the units [w share, (w + 1) share) of the requests one after the other.
+// Every workgroup of a KV head takes the same share of all requests' work, counted in pages: workgroup w the units [w share,
+// (w + 1) share) of the requests one after the other.  A request is `lead` units that stand for what its start costs a workgroup
+// that has another request's pages before it, its pages, and one unit for the new keys.
 struct Share {
-  int share, c, skip;  // units a workgroup; its first request, and the units of that which others take
+  int share, c, skip;   // units a workgroup; its first request, and the units of that which stand before its own
+  int lens, lens_from;  // ctx_len of request lens_from + lane, of some requests from the first on
   bool any;
 };
-__device__ __forceinline__ Share share_of(const int32_t* ctx_len, int C, int max_pages, int w, int n_wgs, int least, int lane) {
+__device__ __forceinline__ Share share_of(const int32_t* ctx_len, int C, int max_pages, int w, int n_wgs, int least, int lead, int lane) {
   const int per = (C + 63) / 64;
+  Share s;
+  s.lens = 0;
+  s.lens_from = 0;
   int mine = 0;
   for (int i = 0; i < per; ++i) {
     const int c = lane * per + i;
-    mine += c < C ? pages_of(clamp_len(ctx_len[c], max_pages)) + 1 : 0;
+    if (c < C) s.lens = ctx_len[c];
+    mine += c < C ? pages_of(clamp_len(s.lens, max_pages)) + lead + 1 : 0;
   }
-  int end = scan_lanes(mine, lane);
+  int end = scan_lanes(mine);
   const int total = __builtin_amdgcn_readlane(end, 63);
-  Share s;
   s.share = (total + n_wgs - 1) / n_wgs;
   s.share = s.share < least ? least : s.share;
   const int64_t at64 = (int64_t)w * s.share;
@@ -231,8 +254,10 @@ __device__ __forceinline__ Share share_of(const int32_t* ctx_len, int C, int max
   s.c = l * per;
   if (per > 1) {
     const int c = s.c + lane;
-    mine = lane < per && c < C ? pages_of(clamp_len(ctx_len[c], max_pages)) + 1 : 0;
-    end = before + scan_lanes(mine, lane);
+    s.lens_from = s.c;
+    s.lens = c < C ? ctx_len[c] : 0;
+    mine = lane < per && c < C ? pages_of(clamp_len(s.lens, max_pages)) + lead + 1 : 0;
+    end = before + scan_lanes(mine);
     l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(end > at));
     before = __builtin_amdgcn_readlane(end - mine, l);
     s.c += l;
@@ -251,35 +276,69 @@ __device__ __forceinline__ void wait_slots(int pending) {  // until at most `pen
   }
 }
 
-// Workgroup = (share of the work, KV head), four waves.  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that share the
-// KV head (row = depth * group + head); PARTS waves with different rows make a stream, and the streams take a request's pages in
-// turn.  A stream has a ring of slots in LDS, filled by its waves some slots ahead of their use.  With one wave a stream (up to 32
-// rows, at D = 64 up to 64) a wave waits for its own copies only and the loop has no barrier; more rows share what a stream copies,
-// which costs a barrier a slot.  At the end of a request's pages the streams' sums are merged through LDS, and leave the results
-// where the request is one workgroup's, otherwise a partial record.
+// A value that the compiler keeps in scalar registers rather than loading it again: a kernel's parameters, all loaded at its start
+// (each first use of a line of them waits for memory), and none in the loops.
+template <class T>
+__device__ __forceinline__ T held(T x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
+// Workgroup = (share of the work, KV head).  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that share the KV head (row =
+// depth * group + head); PARTS waves with different rows make a stream, and the streams take a request's pages in turn.  A stream
+// has a ring of slots in LDS (32 tokens each), filled by its waves some slots ahead of their use.  With one wave a stream (up to
+// 32 rows, at D = 64 up to 64) a wave waits for its own copies only and the loop has no barrier; more rows share what a stream
+// copies, which costs a barrier a slot.  At the end of a request's pages the streams' sums are merged through LDS, and leave the
+// results where the request is one workgroup's, otherwise a partial record.
+template <int D, int RB>
+constexpr int kWavesOf = D == 64 && RB == 1 ? 8 : 4;  // of a workgroup, two workgroups a CU: 128 KiB of rings
 template <int D, bool E5M2, int RB, int PARTS>
-__global__ __launch_bounds__(kWaves * 64, 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
-  constexpr int kSubKeys = 4096 / D, kSubs = kKeysPerTile / kSubKeys;  // keys of a slot; slots of a page
-  constexpr int kNewKeys = 2048 / D;                                   // new keys of a slot
-  constexpr int kStreams = kWaves / PARTS, kDepth = 2 * PARTS, kPer = 8 / PARTS;  // slots of a ring; copies a wave issues for one
-  constexpr int kAhead = PARTS == 1 ? kDepth : kDepth - 1;             // slots on their way or in use
-  const DecodeParams& p = sp.d;
-  __shared__ __attribute__((aligned(16))) char ring[kStreams][kDepth][kSlotBytes];
-  __shared__ float stats[kWaves][RB * 32][2];  // of each wave's rows: reference, sum
+__global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
+  constexpr int kWaves = kWavesOf<D, RB>, kHalf = 32 * D, kSlot = 2 * kHalf;  // bytes of a slot's keys, of a slot
+  constexpr int kStreams = kWaves / PARTS, kDepth = 65536 / kSlot / kStreams;  // slots of a ring
+  constexpr int kCopies = kSlot / 1024 / PARTS;                               // of a slot, by each of a stream's waves
+  constexpr int kAhead = PARTS == 1 ? kDepth : kDepth - 1;                    // slots on their way or in use
+  __shared__ __attribute__((aligned(16))) char ring[kStreams][kDepth][kSlot];
+  __shared__ f32x4 stats[kWaves][RB * 32];  // of each wave's rows: reference, the two sums
   __shared__ int wave_bad[kWaves];
 
+  DecodeParams p = sp.d;
+  p.q_new = held(p.q_new);
+  p.k_new = held(p.k_new);
+  p.v_new = held(p.v_new);
+  p.block_table = held(p.block_table);
+  p.ctx_len = held(p.ctx_len);
+  p.o = held(p.o);
+  p.lse = held(p.lse);
+  p.status = held(p.status);
+  p.part_o = held(p.part_o);
+  p.part_ml = held(p.part_ml);
+  p.C = held(p.C);
+  p.K = held(p.K);
+  p.Hq = held(p.Hq);
+  p.Hkv = held(p.Hkv);
+  p.n_pages = held(p.n_pages);
+  p.max_pages = held(p.max_pages);
+  p.rows_pad = held(p.rows_pad);
+  p.group = held(p.group);
+  p.group_reciprocal = held(p.group_reciprocal);
+  p.c_log2 = held(p.c_log2);
+  const uint8_t *k_pages = held(sp.k_pages), *v_pages = held(sp.v_pages), *k_scale = held(sp.k_scale), *v_scale = held(sp.v_scale);
+  int2* pieces = held(sp.pieces);
+  const int shares = held(sp.shares), least_share = held(sp.least_share), lead = held(sp.lead);
+
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 5, ln = lane & 31;
-  const int kvh = blockIdx.y, part = wave % PARTS, stream = wave / PARTS;
+  const int kvh = blockIdx.y, part = wave % PARTS, stream = wave / PARTS, n_groups = gridDim.x;
   const int n_rows = p.K * p.group;
 
-  int c = blockIdx.x, skip = 0, left = INT_MAX, share = 0;
-  if (sp.shares > 0) {
-    const Share s = share_of(p.ctx_len, p.C, p.max_pages, blockIdx.x, sp.shares, sp.least_share, lane);
+  Share s{0, (int)blockIdx.x, 0, 0, -64, true};
+  int left = INT_MAX;
+  if (shares > 0) {
+    s = share_of(p.ctx_len, p.C, p.max_pages, blockIdx.x, shares, least_share, lead, lane);
     if (!s.any) return;
-    c = s.c;
-    skip = s.skip;
-    left = share = s.share;
+    left = s.share;
   }
+  int c = s.c, skip = s.skip;
 
   int k_off[D / 32], v_off[D / 32];
   {
@@ -297,45 +356,53 @@ __global__ __launch_bounds__(kWaves * 64, 2) void draft_scaled_kernel(ScaledDeco
   for (int b = 0; b < 2; ++b)
     voff[b] = (uint32_t)((lane / kLanes) * D + ((lane % kLanes ^ swz8<D>(b * (64 / kLanes) + lane / kLanes)) << 4));
   const uint32_t ring_at = lds_scalar_addr(&ring[stream][0][0]);
-  // This wave's copies of a slot: f(which half, block of 1 KiB).
+  // This wave's copies of a slot: f(values rather than keys?, block of 1 KiB).
   auto each_copy = [&](auto f) {
     if constexpr (PARTS == 1) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b) f(false, b);
+      for (int b = 0; b < kCopies / 2; ++b) f(false, b);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) f(true, b);
+      for (int b = 0; b < kCopies / 2; ++b) f(true, b);
     } else {
-      const int b0 = part % (PARTS / 2) * kPer;
+      const int b0 = part % (PARTS / 2) * kCopies;
 #pragma unroll
-      for (int b = 0; b < kPer; ++b) f(part >= PARTS / 2, b0 + b);
+      for (int b = 0; b < kCopies; ++b) f(part >= PARTS / 2, b0 + b);
     }
   };
 
-  for (int segment = 0;; ++segment) {
-    int n_ctx = p.ctx_len[c];
+  for (int segment = 0;;) {
+    int n_ctx;
+    if ((unsigned)(c - s.lens_from) < 64u) n_ctx = __builtin_amdgcn_readlane(s.lens, c - s.lens_from);
+    else n_ctx = __builtin_amdgcn_readfirstlane(p.ctx_len[c + (lane_id() & 0)]);  // (by a vector load: no scalar one in a loop)
     bool bad = n_ctx < 0 || n_ctx > p.max_pages * kKeysPerTile;
     n_ctx = clamp_len(n_ctx, p.max_pages);
-    const int n_pg = pages_of(n_ctx), units = n_pg + 1;
-    const int n_units = units - skip < left ? units - skip : left;
-    const int p0 = skip, p1 = skip + n_units < n_pg ? skip + n_units : n_pg;
-    const bool has_new = skip + n_units == units, whole = n_units == units;
+    const int n_pg = pages_of(n_ctx), units = lead + n_pg + 1;
+    const int n_units = units - skip < left ? units - skip : left, to = skip + n_units;
+    if (to <= lead) return;  // (the share ends before the request's pages)
+    const int p0 = skip > lead ? skip - lead : 0, p1 = to - lead < n_pg ? to - lead : n_pg;
+    const bool has_start = skip <= lead, has_new = to == units, whole = has_start && has_new;
 
     Rows<D, RB> r;
     int depth[RB];
-    const int lane_here = lane_id();
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const int row = (part * RB + rb) * 32 + (lane_here & 31);
-      depth[rb] = row < n_rows ? small_quotient(row, p.group_reciprocal) : 0;
-      const int head = kvh * p.group + (row < n_rows ? row - depth[rb] * p.group : 0);
-      const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 16 * (lane_here >> 5);
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + (i / 2) * 32 + (i % 2) * 8));
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) r.o[rb][db] = zero16();
       r.m[rb] = -3.402823466e38f;  // (any score is above it, and it less any score is no NaN)
-      r.l[rb] = 0.f;
+      r.l[rb] = r.w[rb] = 0.f;
     }
+    auto load_queries = [&] {
+      const int l = lane_id();
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int row = (part * RB + rb) * 32 + (l & 31);
+        depth[rb] = row < n_rows ? small_quotient(row, p.group_reciprocal) : 0;
+        const int head = kvh * p.group + (row < n_rows ? row - depth[rb] * p.group : 0);
+        const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 16 * (l >> 5);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + (i / 2) * 32 + (i % 2) * 8));
+      }
+    };
 
     // The last stream's slots hold the new keys first.
     const int n_new = has_new ? (p.K + kNewKeys - 1) / kNewKeys : 0, my_new = stream == kStreams - 1 ? n_new : 0;
@@ -345,179 +412,198 @@ __global__ __launch_bounds__(kWaves * 64, 2) void draft_scaled_kernel(ScaledDeco
     const int n_pages_0 = (p1 - p0 + kStreams - 1) / kStreams;  // pages of stream 0, the most
     const int n_mine = p1 - p0 > stream ? (p1 - p0 - stream + kStreams - 1) / kStreams : 0;
 
-    for (int first = 0; first == 0 || first < n_pages_0; first += 64) {
-      // This stream's next pages, one a lane: page, keys present (0: page id outside the pool), scales.
+    // This stream's pages, 64 at a time, one a lane: page, keys present (0: page id outside the pool), scales.  With them their
+    // copies are begun: slots [0, q0) hold new keys, n_q slots in all.
+    int page, keys, kcode, vcode, q0, n_q, issued;
+    auto copy = [&](int q) {
+      const uint32_t dst = ring_at + (uint32_t)(q & (kDepth - 1)) * kSlot;
+      if (q < q0) {
+        const int l = lane_id();
+        each_copy([&](bool half, int b) {
+          const int row = b * (512 / D) + l / (D / 8), key = q * kNewKeys + row;
+          const uint32_t off = (uint32_t)(key < p.K ? key : p.K - 1) * (uint32_t)(p.Hkv * D * 2) + ((l % (D / 8) ^ swz<D>(row)) << 4);
+          dma16_untracked(half ? v_new : k_new, off, dst + (half ? kHalf : 0) + b * 1024);
+        });
+        return;
+      }
+      const int j = (q - q0) / 2, sub = (q - q0) % 2;
+      const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (2 * kHalf) + sub * kHalf;
+      const int present = __builtin_amdgcn_readlane(keys, j) - sub * 32;
+      if (present >= 32) {
+        each_copy([&](bool half, int b) {
+          dma16_untracked(uniform_ptr((half ? v_pages : k_pages) + at) + b * 1024, voff[b & 1], dst + (half ? kHalf : 0) + b * 1024);
+        });
+      } else {  // rows behind the last token are read as that token: they are masked, and zero times its values adds nothing
+        const int last = present > 0 ? present - 1 : 0, l = lane_id();
+        each_copy([&](bool half, int b) {
+          const int row = b * (64 / kLanes) + l / kLanes;
+          const uint32_t off = (uint32_t)((row < last ? row : last) * D + ((l % kLanes ^ swz8<D>(row)) << 4));
+          dma16_untracked(uniform_ptr((half ? v_pages : k_pages) + at), off, dst + (half ? kHalf : 0) + b * 1024);
+        });
+      }
+    };
+    auto take_pages = [&](int first, int n_before) {
       const int pi = p0 + stream + kStreams * (first + lane_id());
       const bool there = pi < p1;
-      int page = there ? p.block_table[(size_t)c * p.max_pages + pi] : 0;
+      page = there ? p.block_table[(size_t)c * p.max_pages + pi] : 0;
+      if (first == 0) {  // (what the lookup of the pages takes, the queries take too)
+        __builtin_amdgcn_sched_barrier(0);
+        load_queries();
+      }
       const bool fine = page >= 0 && page < p.n_pages;
       bad |= !fine;
       page = fine ? page : 0;
       const int keys_here = n_ctx - pi * kKeysPerTile;
-      const int keys = !there || !fine ? 0 : keys_here < kKeysPerTile ? keys_here : kKeysPerTile;
-      int kcode = 0, vcode = 0;
+      keys = !there || !fine ? 0 : keys_here < kKeysPerTile ? keys_here : kKeysPerTile;
+      kcode = vcode = 0;
       if (there) {
-        kcode = sp.k_scale[(size_t)page * p.Hkv + kvh];
-        vcode = sp.v_scale[(size_t)page * p.Hkv + kvh];
+        kcode = k_scale[(size_t)page * p.Hkv + kvh];
+        vcode = v_scale[(size_t)page * p.Hkv + kvh];
       }
       const int n_here = n_mine - first < 64 ? n_mine - first : 64;
-      const int q0 = first == 0 ? my_new : 0, n_q = q0 + (n_here > 0 ? n_here * kSubs : 0);  // slots: new keys', all
-
-      auto copy = [&](int q) {
-        const uint32_t dst = ring_at + (uint32_t)(q % kDepth) * kSlotBytes;
-        if (q < q0) {
-          const int l = lane_id();
-          each_copy([&](bool half, int b) {
-            const int row = b * (512 / D) + l / (D / 8), key = q * kNewKeys + row;
-            const uint32_t off = (uint32_t)(key < p.K ? key : p.K - 1) * (uint32_t)(p.Hkv * D * 2) + ((l % (D / 8) ^ swz<D>(row)) << 4);
-            dma16_untracked(half ? v_new : k_new, off, dst + (half ? 4096 : 0) + b * 1024);
-          });
-          return;
-        }
-        const int j = (q - q0) / kSubs, sub = (q - q0) % kSubs;
-        const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (kKeysPerTile * D) + sub * 4096;
-        const int present = __builtin_amdgcn_readlane(keys, j) - sub * kSubKeys;
-        if (present >= kSubKeys) {
-          each_copy([&](bool half, int b) {
-            dma16_untracked(uniform_ptr((half ? sp.v_pages : sp.k_pages) + at) + b * 1024, voff[b & 1], dst + (half ? 4096 : 0) + b * 1024);
-          });
-        } else {  // rows behind the last token are read as that token: they are masked, and zero times its values adds nothing
-          const int last = present > 0 ? present - 1 : 0, l = lane_id();
-          each_copy([&](bool half, int b) {
-            const int row = b * (64 / kLanes) + l / kLanes;
-            const uint32_t off = (uint32_t)((row < last ? row : last) * D + ((l % kLanes ^ swz8<D>(row)) << 4));
-            dma16_untracked(uniform_ptr((half ? sp.v_pages : sp.k_pages) + at), off, dst + (half ? 4096 : 0) + b * 1024);
-          });
-        }
-      };
-      int issued = 0;
-      for (; issued < kAhead && issued < n_q; ++issued) copy(issued);
+      q0 = n_before;
+      n_q = q0 + (n_here > 0 ? n_here * 2 : 0);
+      for (issued = 0; issued < 2 && issued < n_q; ++issued) copy(issued);
       __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own loads: none is waited for in the loop, behind its copies)
-      // A slot's turn: what it holds has landed; with several waves a stream, everyone is done with the slot before it, which is
-      // filled again.
-      auto begin = [&](int q) {
-        if (q < n_q) wait_slots<kAhead - 1, kPer>(issued - 1 - q);
-        if (PARTS > 1) {
-          __syncthreads();
-          if (issued < n_q) copy(issued++);
-        }
-      };
-      auto end = [&] {
-        if (PARTS > 1) return;
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot's last reads have left it
+      for (; issued < kAhead && issued < n_q; ++issued) copy(issued);
+    };
+    // A slot's turn: what it holds has landed; with several waves a stream, everyone is done with the slot before it, which is
+    // filled again.
+    auto begin = [&](int q) {
+      wait_slots<kAhead - 1, kCopies>(issued - 1 - q);
+      if (PARTS > 1) {
+        __syncthreads();
         if (issued < n_q) copy(issued++);
-      };
-      int q = 0;
-      if (first == 0) {
-        // (where streams meet at barriers, the others wait for the new keys' turns)
-        for (int i = 0; i < (PARTS > 1 ? n_new : my_new); ++i) {
-          if (my_new == 0) {
-            if (PARTS > 1) __syncthreads();
-            continue;
-          }
-          begin(q);
-          new_keys<D, RB>(r, ring[stream][q % kDepth], q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
-          end();
-          ++q;
-        }
       }
-      const int rounds = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) * kSubs : n_q - q0;
+    };
+    auto end = [&] {
+      if (PARTS > 1) return;
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot's last reads have left it
+      if (issued < n_q) copy(issued++);
+    };
+
+    take_pages(0, my_new);
+    int q = 0;
+    // (where streams meet at barriers, the others wait for the new keys' turns)
+    for (int i = 0; i < (PARTS > 1 ? n_new : my_new); ++i) {
+      if (my_new > 0) begin(q);
+      else if (PARTS > 1) __syncthreads();
+      if (my_new > 0) {
+        new_keys<D, RB>(r, ring[stream][q & (kDepth - 1)], q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+        end();
+        ++q;
+      }
+    }
+    for (int first = 0;;) {
+      const int rounds = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) * 2 : n_q - q0;
       for (int i = 0; i < rounds; ++i, ++q) {
         begin(q);
-        if (q < n_q) {
-          const int j = i / kSubs, visible = __builtin_amdgcn_readlane(keys, j) - i % kSubs * kSubKeys;
-          const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
-          const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(vcode, j) << 23);
-          cached_keys<D, E5M2, RB>(r, ring[stream][q % kDepth], k_off, v_off, ks, vs, visible, g, p.c_log2);
-        }
+        const int j = i / 2, n = __builtin_amdgcn_readlane(keys, j) - i % 2 * 32;  // (0 behind this stream's pages)
+        const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
+        const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(vcode, j) << 23);
+        if (n > 0) cached_keys<D, E5M2, RB>(r, ring[stream][q & (kDepth - 1)], k_off, v_off, ks, vs, n, g, p.c_log2);
         end();
       }
       if (PARTS > 1) __syncthreads();  // (the slots' last reads have left them)
+      first += 64;
+      if (first >= n_pages_0) break;
+      take_pages(first, 0);
+      q = 0;
     }
 
-    // Merge of the waves that hold the same rows: each leaves reference, sum and O (32 rows at a time, in its part of the rings, 16
-    // bytes of features by 16 bytes, the rows of feature group d4 in the order row ^ d4), and the threads add them up in order.
-    bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const float l = sum_halves(r.l[rb]);
-      if (g == 0) {
-        stats[wave][rb * 32 + ln][0] = r.m[rb];
-        stats[wave][rb * 32 + ln][1] = l;
-      }
-    }
-    if (lane == 0) wave_bad[wave] = bad;
-    constexpr int kRegion = 2 * kSlotBytes / 16;
-    static_assert(32 * D / 4 <= kRegion, "32 rows of O must fit a wave's part of the rings");
-    f32x4* regions = reinterpret_cast<f32x4*>(&ring[0][0][0]);
+    // Merge of the streams' waves with the same rows.  Each leaves its references and sums, learns the common ones, leaves its O
+    // against those (in its part of the rings, 16 bytes of features by 16 bytes, the rows of feature group d4 in the order row ^ d4),
+    // and the threads add them up in order.
     const int l = lane_id();
-    const size_t rec = ((size_t)kvh * gridDim.x + blockIdx.x) * 2 + (segment > 0 ? 1 : 0);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      if (rb > 0) __syncthreads();
+      const float a = sum_halves(r.l[rb]), b = sum_halves(r.w[rb]);
+      if (l < 32) stats[wave][rb * 32 + l] = f32x4{r.m[rb], a, b, 0.f};
+    }
+    if (l == 0) wave_bad[wave] = 0;
+    if (__builtin_amdgcn_ballot_w64(bad) != 0 && l == 0) wave_bad[wave] = 1;
+    __syncthreads();
+    int any_bad = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) any_bad |= wave_bad[w];
+    const size_t rec = ((size_t)kvh * n_groups + blockIdx.x) * 2 + (segment > 0 ? 1 : 0);
+    constexpr int kRegion = RB * 32 * D / 4;
+    static_assert(kWaves * kRegion * 16 <= (int)sizeof(ring), "the rows' O must fit a wave's part of the rings");
+    f32x4* regions = reinterpret_cast<f32x4*>(&ring[0][0][0]);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int at = rb * 32 + (l & 31), row = part * RB * 32 + at;
+      float M = r.m[rb], L = 0.f, W = 0.f;
+#pragma unroll
+      for (int i = 0; i < kStreams; ++i) M = __builtin_fmaxf(M, stats[i * PARTS + part][at][0]);
+#pragma unroll
+      for (int i = 0; i < kStreams; ++i) {
+        const f32x4 x = stats[i * PARTS + part][at];
+        const float f = exp2_fast(x[0] - M);
+        L = __builtin_fmaf(x[1], f, L);
+        W = __builtin_fmaf(x[2], f, W);
+      }
+      if (stream == 0 && l < 32) {
+        if (whole) {
+          if (row < n_rows) {
+            const int dep = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - dep * p.group);
+            p.lse[((size_t)c * p.Hq + head) * p.K + dep] = (M + __builtin_log2f(L)) * kLn2;
+          }
+        } else if (row < p.rows_pad) {
+          reinterpret_cast<f32x4*>(p.part_ml)[rec * p.rows_pad + row] = f32x4{M, L, W, any_bad ? 1.f : 0.f};
+        }
+      }
+      const float turn = exp2_fast(r.m[rb] - M) * (whole ? 1.0f / W : 1.0f);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
           const int d4 = db * 8 + 2 * i4 + (l >> 5);
-          regions[wave * kRegion + d4 * 32 + ((l ^ d4) & 31)] =
-              f32x4{r.o[rb][db][4 * i4], r.o[rb][db][4 * i4 + 1], r.o[rb][db][4 * i4 + 2], r.o[rb][db][4 * i4 + 3]};
+          const f32x16& o = r.o[rb][db];
+          regions[wave * kRegion + (rb * (D / 4) + d4) * 32 + ((l ^ d4) & 31)] =
+              f32x4{o[4 * i4] * turn, o[4 * i4 + 1] * turn, o[4 * i4 + 2] * turn, o[4 * i4 + 3] * turn};
         }
-      __syncthreads();
-      const bool any_bad = (wave_bad[0] | wave_bad[1] | wave_bad[2] | wave_bad[3]) != 0;
-      for (int item = wave * 64 + l; item < 32 * PARTS * (D / 4); item += kWaves * 64) {
-        const int d4 = item % (D / 4), in_block = item / (D / 4) % 32, h = item / (32 * (D / 4));
-        const int row = (h * RB + rb) * 32 + in_block;
-        float M = stats[h][rb * 32 + in_block][0];
+    }
+    __syncthreads();
+    constexpr int kItems = 32 * RB * PARTS * (D / 4) / (kWaves * 64);
+#pragma unroll 4
+    for (int k = 0; k < kItems; ++k) {
+      const int item = (k * kWaves + wave) * 64 + l;
+      const int d4 = item % (D / 4), row = item / (D / 4), at = row % (RB * 32), h = row / (RB * 32);
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 1; s < kStreams; ++s) M = __builtin_fmaxf(M, stats[s * PARTS + h][rb * 32 + in_block][0]);
-        float L = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < kStreams; ++s) {
-          const int w = s * PARTS + h;
-          const float f = exp2_fast(stats[w][rb * 32 + in_block][0] - M);
-          L = __builtin_fmaf(stats[w][rb * 32 + in_block][1], f, L);
-          o += regions[w * kRegion + d4 * 32 + (in_block ^ (d4 & 31))] * f;
+      for (int i = 0; i < kStreams; ++i) o += regions[(i * PARTS + h) * kRegion + (at / 32 * (D / 4) + d4) * 32 + ((at ^ d4) & 31)];
+      if (whole) {
+        if (row < n_rows) {
+          const int dep = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - dep * p.group);
+          u32x2 out;
+          out[0] = pack_bf16(o[0], o[1]);
+          out[1] = pack_bf16(o[2], o[3]);
+          *reinterpret_cast<u32x2*>(p.o + (((size_t)c * p.K + dep) * p.Hq + head) * D + d4 * 4) = out;
         }
-        if (whole) {
-          if (row < n_rows) {
-            const int dep = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - dep * p.group);
-            const float inv = 1.0f / L;
-            u32x2 out;
-            out[0] = pack_bf16(o[0] * inv, o[1] * inv);
-            out[1] = pack_bf16(o[2] * inv, o[3] * inv);
-            *reinterpret_cast<u32x2*>(p.o + (((size_t)c * p.K + dep) * p.Hq + head) * D + d4 * 4) = out;
-            if (d4 == 0) p.lse[((size_t)c * p.Hq + head) * p.K + dep] = (M + __builtin_log2f(L)) * kLn2;
-          }
-        } else if (row < p.rows_pad) {
-          *reinterpret_cast<f32x4*>(p.part_o + (rec * p.rows_pad + row) * D + d4 * 4) = o;
-          if (d4 == 0) {
-            float* ml = p.part_ml + rec * 3 * p.rows_pad + row;
-            ml[0] = M;
-            ml[p.rows_pad] = L;
-            ml[2 * p.rows_pad] = any_bad ? 1.f : 0.f;
-          }
-        }
-      }
-      if (rb == 0 && tid == 0 && kvh == 0) {
-        if (whole && p.status) p.status[c] = any_bad;
-        // where the request's records stand: the first, and how many workgroups leave one
-        if (share > 0 && skip == 0) sp.pieces[c] = make_int2((int)blockIdx.x * 2 + (segment > 0 ? 1 : 0), 1 + (units - n_units + share - 1) / share);
+      } else if (row < p.rows_pad) {
+        *reinterpret_cast<f32x4*>(p.part_o + (rec * p.rows_pad + row) * D + d4 * 4) = o;
       }
     }
+    if (tid == 0 && kvh == 0) {
+      if (whole && p.status) p.status[c] = any_bad;
+      // where the request's records stand: the first, and how many workgroups leave one
+      if (s.share > 0 && has_start) pieces[c] = make_int2((int)blockIdx.x * 2 + (segment > 0 ? 1 : 0), 1 + (units - to + s.share - 1) / s.share);
+    }
+    ++segment;
     left -= n_units;
     skip = 0;
-    if (sp.shares == 0 || ++c >= p.C || left <= 0) return;
+    if (shares == 0 || ++c >= p.C || left <= 0) return;
     __syncthreads();  // the merge's reads have left the rings
   }
 }
 
-// Merges a request's partial records: M = max m_s, L = sum l_s 2^(m_s - M), O = sum O_s 2^(m_s - M) / L.  kLanes threads per (row,
-// 4 features) take the records in turn, kEach at a time, whose loads are issued before the first is used.
+// Merges a request's partial records: M = max m_s, each sum and O the sum of the records' times 2^(m_s - M).  A workgroup takes
+// kRows rows; a row's threads - D / 4 for its features, kLanes of them for the records in turn - look at kEach records at a time,
+// whose loads are issued before the first is used.
 template <int D>
 __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeParams sp) {
-  constexpr int kLanes = 256 / D, kEach = 4;
+  constexpr int kLanes = 256 / D, kEach = 8;
   const DecodeParams& p = sp.d;
   const int lane = threadIdx.x & 63, d4 = lane % (D / 4), sl = lane / (D / 4);
   const int kvh = blockIdx.y, c = blockIdx.z, n_rows = p.K * p.group;
@@ -529,43 +615,44 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
   // record 0 may be its workgroup's second, the others are their workgroups' first
   const size_t rec0 = (size_t)kvh * sp.shares * 2;
   auto record = [&](int s) { return rec0 + (s == 0 ? piece.x : (piece.x / 2 + s) * 2); };
-  float M = -3.402823466e38f, L = 0.f;
+  float M = -3.402823466e38f, L = 0.f, W = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   bool bad = false;
   for (int s0 = 0; s0 < n; s0 += kLanes * kEach) {
-    float mv[kEach], lv[kEach], fv[kEach];
-    f32x4 ov[kEach];
+    f32x4 ml[kEach], ov[kEach];
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {  // (records past the last are read as the last and weigh nothing)
+    for (int j = 0; j < kEach; ++j) {  // (records past the last are read as the last)
       const int s = s0 + j * kLanes + sl;
-      const size_t rec = record(s < n ? s : n - 1);
-      const float* ml = p.part_ml + rec * 3 * p.rows_pad + row;
-      mv[j] = ml[0];
-      lv[j] = ml[p.rows_pad];
-      fv[j] = ml[2 * p.rows_pad];
-      ov[j] = *reinterpret_cast<const f32x4*>(p.part_o + (rec * p.rows_pad + row) * D + d4 * 4);
+      const size_t at = record(s < n ? s : n - 1) * p.rows_pad + row;
+      ml[j] = reinterpret_cast<const f32x4*>(p.part_ml)[at];
+      ov[j] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + d4 * 4);
     }
     float m_new = M;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) m_new = __builtin_fmaxf(m_new, mv[j]);
+    for (int j = 0; j < kEach; ++j) m_new = __builtin_fmaxf(m_new, ml[j][0]);
     const float turn = exp2_fast(M - m_new);
     M = m_new;
     L *= turn;
+    W *= turn;
     acc *= turn;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-      const float w = s0 + j * kLanes + sl < n ? exp2_fast(mv[j] - M) : 0.f;
-      L = __builtin_fmaf(lv[j], w, L);
-      acc += ov[j] * w;
-      bad |= fv[j] != 0.f;
+      if (s0 + j * kLanes + sl < n) {  // (not by a weight of zero: a record may hold infinities)
+        const float w = exp2_fast(ml[j][0] - M);
+        L = __builtin_fmaf(ml[j][1], w, L);
+        W = __builtin_fmaf(ml[j][2], w, W);
+        acc += ov[j] * w;
+        bad |= ml[j][3] != 0.f;
+      }
     }
   }
 #pragma unroll
   for (int x = D / 4; x < 64; x <<= 1) {
-    const float m_other = __shfl_xor(M, x), l_other = __shfl_xor(L, x), m_new = __builtin_fmaxf(M, m_other);
+    const float m_other = __shfl_xor(M, x), m_new = __builtin_fmaxf(M, m_other);
     const float a = exp2_fast(M - m_new), b = exp2_fast(m_other - m_new);
     M = m_new;
-    L = L * a + l_other * b;
+    L = L * a + __shfl_xor(L, x) * b;
+    W = W * a + __shfl_xor(W, x) * b;
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + __shfl_xor(acc[j], x) * b;
   }
@@ -574,7 +661,7 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
     if (lane == 0) p.status[c] = any;
   }
   if (sl != 0) return;
-  const float inv = 1.0f / L;
+  const float inv = 1.0f / W;
   const int depth = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - depth * p.group);
   u32x2 out;
   out[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
@@ -584,35 +671,54 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
 }
 
 constexpr int kCus = 256;  // compute units of the device
-constexpr int kLeastShare = 8;  // pages
+// Streams of a workgroup for rows in `blocks` of 32.
+int streams_of(int D, int blocks) {
+  if (D == 64) return blocks == 1 ? 8 : blocks == 2 ? 4 : 2;
+  return blocks == 1 ? 4 : blocks == 2 ? 2 : 1;
+}
 
 }  // namespace
 
-// Workgroups that share the work of a KV head, 0: a workgroup for each request.
-int draft_scaled_shares(int C, int Hkv, int max_pages) {
-  if (C > 1024 || max_pages < kLeastShare || (int64_t)C * (max_pages + 1) > INT_MAX) return 0;
-  const int64_t slots = (2 * kCus + Hkv - 1) / Hkv, most = ((int64_t)C * (max_pages + 1) + kLeastShare - 1) / kLeastShare;
-  return (int)(slots < most ? slots : most);
+// Units a workgroup takes at least, and units that the start of a request counts for.
+#ifndef LEASTP
+#define LEASTP 2
+#endif
+#ifndef LEADP
+#define LEADP 8
+#endif
+ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
+  ShareRule r;
+  r.least = LEASTP * streams_of(D, blocks);
+  r.lead = LEADP;
+  r.shares = 0;
+  const int64_t most = (int64_t)C * (max_pages + r.lead + 1);
+  if (C > 1024 || max_pages <= r.least || most > INT_MAX) return r;  // a workgroup for each request
+  const int64_t slots = (2 * kCus + Hkv - 1) / Hkv, useful = (most + r.least - 1) / r.least;
+  r.shares = (int)(slots < useful ? slots : useful);
+  return r;
 }
 
 hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, hipStream_t stream) {
   ScaledDecodeParams p = pin;
   p.d.group = p.d.Hq / p.d.Hkv;
   p.d.group_reciprocal = small_reciprocal(p.d.group);
-  p.least_share = kLeastShare;
+  const int blocks = p.d.rows_pad / 32;
+  const ShareRule rule = draft_scaled_rule(p.d.C, p.d.Hkv, p.d.max_pages, blocks, D);
+  p.shares = rule.shares;
+  p.least_share = rule.least;
+  p.lead = rule.lead;
   const dim3 grid((unsigned)(p.shares > 0 ? p.shares : p.d.C), (unsigned)p.d.Hkv);
-  auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), 0, stream, p); };
   auto go = [&](auto type) {
     constexpr bool T = decltype(type)::value;
-    const int blocks = p.d.rows_pad / 32;
+    auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)waves * 64), 0, stream, p); };
     if (D == 64) {
-      if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1>);
-      else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1>);
-      else run(draft_scaled_kernel<64, T, 2, 2>);
+      if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1>, kWavesOf<64, 1>);
+      else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1>, kWavesOf<64, 2>);
+      else run(draft_scaled_kernel<64, T, 2, 2>, kWavesOf<64, 2>);
     } else {
-      if (blocks == 1) run(draft_scaled_kernel<128, T, 1, 1>);
-      else if (blocks == 2) run(draft_scaled_kernel<128, T, 1, 2>);
-      else run(draft_scaled_kernel<128, T, 1, 4>);
+      if (blocks == 1) run(draft_scaled_kernel<128, T, 1, 1>, kWavesOf<128, 1>);
+      else if (blocks == 2) run(draft_scaled_kernel<128, T, 1, 2>, kWavesOf<128, 1>);
+      else run(draft_scaled_kernel<128, T, 1, 4>, kWavesOf<128, 1>);
     }
   };
   e5m2 ? go(std::true_type{}) : go(std::false_type{});
