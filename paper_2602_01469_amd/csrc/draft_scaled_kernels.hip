@@ -679,21 +679,30 @@ int streams_of(int D, int blocks) {
 
 }  // namespace
 
-// Units a workgroup takes at least, and units that the start of a request counts for.
-#ifndef LEASTP
-#define LEASTP 2
-#endif
-#ifndef LEADP
-#define LEADP 8
-#endif
+// How the work of a KV head is shared, from the sizes that the host knows; times as microseconds a step on MI355X, D 64, 8 heads
+// of keys, 7 or 8 rows a position unless noted.
+//   lead   the start of a share (its part of the lookup, queries, merge) takes as long as some 8 pages.
+//   least  two pages a stream, so that each wave has copies under way while it works.
+//   By request, without the second launch: where one request's pages are too few to divide (at most two a stream), and where
+//          eight a stream or fewer meet half the CUs' worth of workgroups: 14.8 against 21.1 for 16 requests of 1000 tokens, 22.0
+//          against 33.0 for 32 of 1000 to 2000; sixteen a stream would help some (51.7 against 57.5 for 64 of 300 to 4000) and
+//          cost others (33.5 against 28.5 for 16 of 2500 to 4000).  With fewer workgroups the pages are divided (D 128, 4 requests
+//          of 768 tokens: 14.1 against 15.8).
+//   shares a workgroup on each CU while each would have fewer than 12 units with two a CU, as the starts and the records weigh
+//          more than the reads in flight: 16.1 against 18.8 for 4 requests of 2048 to 4096, 21.9 against 25.9 for 2 of 10800 to
+//          20000 (D 128), 17.5 against 20.3 for one of 20000.  Above that two: 89.7 against 95.6 for 64 of 512 to 8192, 101
+//          against 117 for 48 of 500 to 8191 (D 128, 128 rows).
 ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
+  const int streams = streams_of(D, blocks);
   ShareRule r;
-  r.least = LEASTP * streams_of(D, blocks);
-  r.lead = LEADP;
+  r.least = 2 * streams;
+  r.lead = 8;
   r.shares = 0;
-  const int64_t most = (int64_t)C * (max_pages + r.lead + 1);
-  if (C > 1024 || max_pages <= r.least || most > INT_MAX) return r;  // a workgroup for each request
-  const int64_t slots = (2 * kCus + Hkv - 1) / Hkv, useful = (most + r.least - 1) / r.least;
+  const int64_t most = (int64_t)C * (max_pages + r.lead + 1);  // units of a KV head
+  if (C > 1024 || max_pages <= 2 * streams || most > INT_MAX) return r;
+  if (max_pages <= 8 * streams && (int64_t)C * Hkv >= kCus / 2) return r;
+  const int per_cu = most * Hkv >= 12 * 2 * kCus ? 2 : 1;
+  const int64_t slots = (per_cu * kCus + Hkv - 1) / Hkv, useful = (most + r.least - 1) / r.least;
   r.shares = (int)(slots < useful ? slots : useful);
   return r;
 }
