@@ -91,21 +91,21 @@ __device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, const f32x16& s, fl
   pb[1] = pack8_sum(x, 1, r.w[rb]);
 }
 
-// The 32 keys of a slot, of which the first n count (the others are masked; their values are finite).
+// 32 keys, staged with their values, of which the first n count (the others are masked; their values are finite).
 template <int D, bool E5M2, int RB>
-__device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* slot, const int (&k_off)[D / 32], const int (&v_off)[D / 32],
-                                            float ks, float vs, int n, int g, float c) {
+__device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, const int (&k_off)[D / 32],
+                                            const int (&v_off)[D / 32], float ks, float vs, int n, int g, float c) {
   // All LDS reads first: one at a time in front of its use, as the compiler places them otherwise, each would be waited for.
   typedef __attribute__((ext_vector_type(2))) int i32x2;
   u32x4 kw[D / 32];
   i32x2 vw[2][D / 32];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) kw[i] = *reinterpret_cast<const u32x4*>(slot + k_off[i]);
+  for (int i = 0; i < D / 32; ++i) kw[i] = *reinterpret_cast<const u32x4*>(k_at + k_off[i]);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
-      vw[t][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(PEAGLE_LDS_PTR(i32x2, slot + 32 * D + v_off[db] + t * 16 * D));
+      vw[t][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(PEAGLE_LDS_PTR(i32x2, v_at + v_off[db] + t * 16 * D));
   __builtin_amdgcn_sched_barrier(0);
   f32x16 s[RB];
 #pragma unroll
@@ -145,15 +145,15 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* slot, co
 // one `stride` elements on).
 constexpr int kNewKeys = 16;
 template <int D, int RB>
-__device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* slot, int k0, int K, const __bf16* v_new, uint32_t stride,
+__device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, int k0, int K, const __bf16* v_new, uint32_t stride,
                                          const int (&depth)[RB], float c) {
   const int lane = lane_id(), g = lane >> 5, row = lane % kNewKeys;
   bf16x8 ka[D / 16], va[D / 32];
   const TrOff<D> to = tr_offsets<D>(lane);
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(slot + tile_off<D>(row, 4 * (i / 2) + 2 * g + i % 2));
+  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(k_at + tile_off<D>(row, 4 * (i / 2) + 2 * g + i % 2));
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) va[db] = frag_tr<D>(slot + 32 * D, to, 0, db);
+  for (int db = 0; db < D / 32; ++db) va[db] = frag_tr<D>(v_at, to, 0, db);
   __builtin_amdgcn_sched_barrier(0);
   f32x16 s[RB];
 #pragma unroll
@@ -294,8 +294,9 @@ template <int D, int RB>
 constexpr int kWavesOf = D == 64 && RB == 1 ? 8 : 4;  // of a workgroup, two workgroups a CU: 128 KiB of rings
 template <int D, bool E5M2, int RB, int PARTS>
 __global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
-  constexpr int kWaves = kWavesOf<D, RB>, kHalf = 32 * D, kSlot = 2 * kHalf;  // bytes of a slot's keys, of a slot
-  constexpr int kStreams = kWaves / PARTS, kDepth = 65536 / kSlot / kStreams;  // slots of a ring
+  constexpr int kWaves = kWavesOf<D, RB>, kStreams = kWaves / PARTS, kRing = 65536 / kStreams;  // waves, streams, bytes of a ring
+  constexpr int kTokens = kRing >= 4 * 64 * D ? 64 : 32, kHalf = kTokens * D, kSlot = 2 * kHalf;  // a slot: bytes of its keys, in all
+  constexpr int kPerPage = kKeysPerTile / kTokens, kDepth = kRing / kSlot;                        // slots of a page, of a ring
   constexpr int kCopies = kSlot / 1024 / PARTS;                               // of a slot, by each of a stream's waves
   constexpr int kAhead = PARTS == 1 ? kDepth : kDepth - 1;                    // slots on their way or in use
   __shared__ __attribute__((aligned(16))) char ring[kStreams][kDepth][kSlot];
@@ -426,10 +427,10 @@ __global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void
         });
         return;
       }
-      const int j = (q - q0) / 2, sub = (q - q0) % 2;
-      const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (2 * kHalf) + sub * kHalf;
-      const int present = __builtin_amdgcn_readlane(keys, j) - sub * 32;
-      if (present >= 32) {
+      const int j = (q - q0) / kPerPage, sub = (q - q0) % kPerPage;
+      const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (kKeysPerTile * D) + sub * kHalf;
+      const int present = __builtin_amdgcn_readlane(keys, j) - sub * kTokens;
+      if (present >= kTokens) {
         each_copy([&](bool half, int b) {
           dma16_untracked(uniform_ptr((half ? v_pages : k_pages) + at) + b * 1024, voff[b & 1], dst + (half ? kHalf : 0) + b * 1024);
         });
@@ -462,8 +463,8 @@ __global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void
       }
       const int n_here = n_mine - first < 64 ? n_mine - first : 64;
       q0 = n_before;
-      n_q = q0 + (n_here > 0 ? n_here * 2 : 0);
-      for (issued = 0; issued < 2 && issued < n_q; ++issued) copy(issued);
+      n_q = q0 + (n_here > 0 ? n_here * kPerPage : 0);
+      for (issued = 0; issued < kPerPage && issued < n_q; ++issued) copy(issued);
       __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own loads: none is waited for in the loop, behind its copies)
       for (; issued < kAhead && issued < n_q; ++issued) copy(issued);
     };
@@ -489,20 +490,26 @@ __global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void
       if (my_new > 0) begin(q);
       else if (PARTS > 1) __syncthreads();
       if (my_new > 0) {
-        new_keys<D, RB>(r, ring[stream][q & (kDepth - 1)], q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+        const char* at = ring[stream][q & (kDepth - 1)];
+        new_keys<D, RB>(r, at, at + kHalf, q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
         end();
         ++q;
       }
     }
     for (int first = 0;;) {
-      const int rounds = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) * 2 : n_q - q0;
-      for (int i = 0; i < rounds; ++i, ++q) {
-        begin(q);
+      const int rounds = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) * 2 : (n_q - q0) * (kTokens / 32);
+      for (int i = 0; i < rounds; ++i) {
+        const bool starts = kTokens == 32 || i % 2 == 0, ends = kTokens == 32 || i % 2 != 0;  // a slot's turn
+        if (starts) begin(q);
         const int j = i / 2, n = __builtin_amdgcn_readlane(keys, j) - i % 2 * 32;  // (0 behind this stream's pages)
         const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
         const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(vcode, j) << 23);
-        if (n > 0) cached_keys<D, E5M2, RB>(r, ring[stream][q & (kDepth - 1)], k_off, v_off, ks, vs, n, g, p.c_log2);
-        end();
+        const char* at = ring[stream][q & (kDepth - 1)] + (kTokens == 32 ? 0 : i % 2 * 32 * D);
+        if (n > 0) cached_keys<D, E5M2, RB>(r, at, at + kHalf, k_off, v_off, ks, vs, n, g, p.c_log2);
+        if (ends) {
+          end();
+          ++q;
+        }
       }
       if (PARTS > 1) __syncthreads();  // (the slots' last reads have left them)
       first += 64;
