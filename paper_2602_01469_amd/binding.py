@@ -603,13 +603,20 @@ def peagle_cache_plan_workspace_bytes(shape: PlanShape) -> int:
     return n
 
 
-def _on_current_device(**tensors) -> None:
-    """The call runs on the current device's stream: its tensors have to be that device's."""
+def _ptr_on(device: int, t, name: str, dtype, shape):
+    """_ptr() of a tensor that has to live on GPU `device`."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device >= 0:
+        return t.data_ptr()
+    _ptr(t, name, dtype, shape)
+    raise ValueError(f"{name}: lives on {t.device}, other tensors of the call on cuda:{device}")
+
+
+def _stream_on(device: int, stream):
+    """_stream_ptr() of a call whose tensors live on GPU `device`: it runs on a stream of the current device."""
     import torch
-    dev = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"{name}: lives on {t.device}, the current device is cuda:{dev}")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors live on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream_ptr(stream)
 
 
 def peagle_cache_plan(shape: PlanShape, ctx_len, new_len, pages_held, free_pages, free_count, block_table, token_start, slots,
@@ -624,17 +631,16 @@ def peagle_cache_plan(shape: PlanShape, ctx_len, new_len, pages_held, free_pages
         free_count_out = free_count
     if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
         raise TypeError("workspace: expected a contiguous uint8 GPU tensor")
-    per_request = (s.C,)
-    args = [_ptr(ctx_len, "ctx_len", i32, per_request), _ptr(new_len, "new_len", i32, per_request),
-            _ptr(pages_held, "pages_held", i32, per_request), _ptr(pages_held_out, "pages_held_out", i32, per_request),
-            _ptr(free_pages, "free_pages", i32, (s.n_pages,)), _ptr(free_count, "free_count", i32, (1,)),
-            _ptr(free_count_out, "free_count_out", i32, (1,)), _ptr(block_table, "block_table", i32, (s.C, s.max_pages)),
-            _ptr(token_start, "token_start", i32, (s.C + 1,)), _ptr(slots, "slots", torch.int64, (s.max_tokens,)),
-            _ptr(seq_len, "seq_len", i32, per_request), _ptr(status, "status", i32, per_request)]
-    _on_current_device(ctx_len=ctx_len, new_len=new_len, pages_held=pages_held, pages_held_out=pages_held_out,
-                       free_pages=free_pages, free_count=free_count, free_count_out=free_count_out, block_table=block_table,
-                       token_start=token_start, slots=slots, seq_len=seq_len, status=status, workspace=workspace)
-    rc = load_library().peagle_cache_plan(s.c(), *args, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    dev, per_request, one = workspace.get_device(), (s.C,), (1,)
+    rc = load_library().peagle_cache_plan(
+        s.c(), _ptr_on(dev, ctx_len, "ctx_len", i32, per_request), _ptr_on(dev, new_len, "new_len", i32, per_request),
+        _ptr_on(dev, pages_held, "pages_held", i32, per_request), _ptr_on(dev, pages_held_out, "pages_held_out", i32, per_request),
+        _ptr_on(dev, free_pages, "free_pages", i32, (s.n_pages,)), _ptr_on(dev, free_count, "free_count", i32, one),
+        _ptr_on(dev, free_count_out, "free_count_out", i32, one),
+        _ptr_on(dev, block_table, "block_table", i32, (s.C, s.max_pages)),
+        _ptr_on(dev, token_start, "token_start", i32, (s.C + 1,)), _ptr_on(dev, slots, "slots", torch.int64, (s.max_tokens,)),
+        _ptr_on(dev, seq_len, "seq_len", i32, per_request), _ptr_on(dev, status, "status", i32, per_request),
+        workspace.data_ptr(), workspace.numel(), _stream_on(dev, stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_cache_plan")
 
@@ -649,45 +655,52 @@ class CacheShape:
 CACHE_E4M3, CACHE_E5M2 = 0, 1
 
 
-def _cache_pools(k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: int, D: int):
-    """Pointers of an 8-bit cache's pools and scales, and its format."""
+def _cache_pools(device, k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: int, D: int):
+    """Format of an 8-bit cache, and the pointers of its pools and scales."""
     import torch
-    formats = {torch.float8_e4m3fn: CACHE_E4M3, torch.float8_e5m2: CACHE_E5M2}
-    if k_pages.dtype not in formats:
-        raise TypeError(f"k_pages: expected torch.float8_e4m3fn or torch.float8_e5m2, got {k_pages.dtype}")
-    if v_pages.dtype != k_pages.dtype:
-        raise TypeError(f"v_pages: expected {k_pages.dtype}, got {v_pages.dtype}")
-    pool, e8 = (n_pages, Hkv, 64, D), torch.float8_e8m0fnu
-    return formats[k_pages.dtype], [_ptr(k_pages, "k_pages", k_pages.dtype, pool), _ptr(v_pages, "v_pages", k_pages.dtype, pool),
-                                    _ptr(k_scale, "k_scale", e8, (n_pages, Hkv)), _ptr(v_scale, "v_scale", e8, (n_pages, Hkv))]
+    kind = k_pages.dtype
+    if kind is torch.float8_e4m3fn:
+        fmt = CACHE_E4M3
+    elif kind is torch.float8_e5m2:
+        fmt = CACHE_E5M2
+    else:
+        raise TypeError(f"k_pages: expected torch.float8_e4m3fn or torch.float8_e5m2, got {kind}")
+    if v_pages.dtype is not kind:
+        raise TypeError(f"v_pages: expected {kind}, got {v_pages.dtype}")
+    pool, scales, e8 = (n_pages, Hkv, 64, D), (n_pages, Hkv), torch.float8_e8m0fnu
+    return (fmt, _ptr_on(device, k_pages, "k_pages", kind, pool), _ptr_on(device, v_pages, "v_pages", kind, pool),
+            _ptr_on(device, k_scale, "k_scale", e8, scales), _ptr_on(device, v_scale, "v_scale", e8, scales))
 
 
-def _rows_ptr(t, name: str, dtype, shape):
-    """Device pointer and row distance (elements) of a tensor whose rows are whole but may stand apart."""
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+def _rows_ptr(device: int, t, name: str, shape):
+    """Device pointer and row distance (elements) of a bf16 tensor whose rows are whole but may stand apart."""
+    import torch
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError(f"{name}: must live on the GPU")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: lives on {t.device}, other tensors of the call on cuda:{device}")
     n, H, D = shape
-    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+    along, across, inner = t.stride()
+    if (D > 1 and inner != 1) or (H > 1 and across != D):
         raise ValueError(f"{name}: a token's heads must be contiguous")
-    return t.data_ptr(), t.stride(0) if n > 1 else H * D
+    return t.data_ptr(), along if n > 1 else H * D
 
 
 def peagle_cache_append_scaled(shape: CacheShape, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream=None) -> None:
     """Stores k_new, v_new [n_tokens, Hkv, D] (a token's heads contiguous, tokens any multiple of 8 elements apart) at `slots`."""
     import torch
-    s = shape
-    fmt, pools = _cache_pools(k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    s, dev = shape, k_pages.get_device()
+    fmt, *pools = _cache_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
     rows = (s.n_tokens, s.Hkv, s.D)
-    k, k_stride = _rows_ptr(k_new, "k_new", torch.bfloat16, rows)
-    v, v_stride = _rows_ptr(v_new, "v_new", torch.bfloat16, rows)
-    at = _ptr(slots, "slots", torch.int64, (s.n_tokens,))
-    _on_current_device(k_new=k_new, v_new=v_new, slots=slots, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale)
+    k, k_stride = _rows_ptr(dev, k_new, "k_new", rows)
+    v, v_stride = _rows_ptr(dev, v_new, "v_new", rows)
+    at = _ptr_on(dev, slots, "slots", torch.int64, (s.n_tokens,))
     c = _CacheShapeC(s.n_tokens, s.Hkv, s.D, s.n_pages, fmt, k_stride, v_stride)
-    rc = load_library().peagle_cache_append_scaled(C.byref(c), k, v, at, *pools, _stream_ptr(stream))
+    rc = load_library().peagle_cache_append_scaled(C.byref(c), k, v, at, *pools, _stream_on(dev, stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_cache_append_scaled")
 
@@ -708,14 +721,15 @@ def peagle_draft_decode_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages,
     s = shape
     if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
         raise TypeError("workspace: expected a contiguous uint8 GPU tensor")
-    fmt, pools = _cache_pools(k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
-    new = (s.C, s.K, s.Hkv, s.D)
-    args = [_ptr(q_new, "q_new", bf, (s.C, s.K, s.Hq, s.D)), _ptr(k_new, "k_new", bf, new), _ptr(v_new, "v_new", bf, new), *pools,
-            _ptr(block_table, "block_table", i32, (s.C, s.max_pages)), _ptr(ctx_len, "ctx_len", i32, (s.C,)),
-            _ptr(o, "o", bf, (s.C, s.K, s.Hq, s.D)), _ptr(lse, "lse", f32, (s.C, s.Hq, s.K)), _ptr(status, "status", i32, (s.C,))]
-    _on_current_device(q_new=q_new, k_new=k_new, v_new=v_new, k_pages=k_pages, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale,
-                       block_table=block_table, ctx_len=ctx_len, o=o, lse=lse, status=status, workspace=workspace)
-    rc = load_library().peagle_draft_decode_scaled(s.c(), fmt, *args, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    dev = workspace.get_device()
+    fmt, *pools = _cache_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    rows, new = (s.C, s.K, s.Hq, s.D), (s.C, s.K, s.Hkv, s.D)
+    rc = load_library().peagle_draft_decode_scaled(
+        s.c(), fmt, _ptr_on(dev, q_new, "q_new", bf, rows), _ptr_on(dev, k_new, "k_new", bf, new), _ptr_on(dev, v_new, "v_new", bf, new),
+        *pools, _ptr_on(dev, block_table, "block_table", i32, (s.C, s.max_pages)), _ptr_on(dev, ctx_len, "ctx_len", i32, (s.C,)),
+        _ptr_on(dev, o, "o", bf, rows), _ptr_on(dev, lse, "lse", f32, (s.C, s.Hq, s.K)),
+        None if status is None else _ptr_on(dev, status, "status", i32, (s.C,)),
+        workspace.data_ptr(), workspace.numel(), _stream_on(dev, stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_draft_decode_scaled")
 
