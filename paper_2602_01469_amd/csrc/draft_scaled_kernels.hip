@@ -283,6 +283,12 @@ __device__ __forceinline__ T held(T x) {
   asm volatile("" : "+s"(x));
   return x;
 }
+template <class T>
+__device__ __forceinline__ T* held(T* x) {  // (as a pointer to global memory, which an opaque pointer is not known to be)
+  __attribute__((address_space(1))) T* g = (__attribute__((address_space(1))) T*)x;
+  asm volatile("" : "+s"(g));
+  return (T*)g;
+}
 
 // Workgroup = (share of the work, KV head).  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that share the KV head (row =
 // depth * group + head); PARTS waves with different rows make a stream, and the streams take a request's pages in turn.  A stream
@@ -464,7 +470,9 @@ __global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void
       const int n_here = n_mine - first < 64 ? n_mine - first : 64;
       q0 = n_before;
       n_q = q0 + (n_here > 0 ? n_here * kPerPage : 0);
-      for (issued = 0; issued < kPerPage && issued < n_q; ++issued) copy(issued);
+      // (one slot's copies with the loads: behind more, the wait for the loads would be one for the slots that are due later)
+      issued = 0;
+      if (n_q > 0) copy(issued++);
       __builtin_amdgcn_s_waitcnt(0x0F70);  // (the compiler's own loads: none is waited for in the loop, behind its copies)
       for (; issued < kAhead && issued < n_q; ++issued) copy(issued);
     };
@@ -724,11 +732,16 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, 
   p.least_share = rule.least;
   p.lead = rule.lead;
   const dim3 grid((unsigned)(p.shares > 0 ? p.shares : p.d.C), (unsigned)p.d.Hkv);
+  // With a workgroup a CU at most, two blocks of rows at D = 64 are two waves' rather than one's: what a wave does for a slot is
+  // the time then (15.0 against 15.9 us for 4 requests of 2048 to 4096 tokens).  With more, widening each value once counts (91
+  // against 94 us for 64 of 512 to 8192).
+  const bool alone = (int64_t)grid.x * grid.y <= kCus;
   auto go = [&](auto type) {
     constexpr bool T = decltype(type)::value;
     auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)waves * 64), 0, stream, p); };
     if (D == 64) {
       if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1>, kWavesOf<64, 1>);
+      else if (blocks == 2 && alone) run(draft_scaled_kernel<64, T, 1, 2>, kWavesOf<64, 1>);
       else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1>, kWavesOf<64, 2>);
       else run(draft_scaled_kernel<64, T, 2, 2>, kWavesOf<64, 2>);
     } else {
