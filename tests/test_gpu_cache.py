@@ -8,6 +8,7 @@ import torch
 import paper_2602_01469_amd as pe
 from gpu_harness import bf16_to_f64
 from oracle import peagle_oracle as orc
+from test_gpu_guards import Guarded
 
 pytestmark = pytest.mark.gpu
 
@@ -181,6 +182,37 @@ def test_plan_replays_from_a_graph():
             p.check(("replay", rep))
 
 
+@pytest.mark.parametrize("C,ctx_hi,new_hi,pad", [(5, 300, 9, 3), (70, 900, 8, 700), (1100, 300, 8, 9001)])
+def test_plan_stays_inside_its_buffers(C, ctx_hi, new_hi, pad):
+    print(f"case plan guards C={C}", flush=True)
+    rng = np.random.default_rng(C)
+    state = _state(rng, C, ctx_hi, new_hi, 1, extra_columns=1)  # (a request may hold one page more than it needs)
+    p = Plan(*state, int(state[1].sum()) + pad)
+    g = Guarded()
+    for name in ("held", "free", "table", "count", "start", "seq_len", "status", "slots", "ws"):
+        x = getattr(p, name)
+        setattr(p, name, g.tensor(name, tuple(x.shape), x.dtype).copy_(x))
+    p.call()
+    g.check("plan")
+    p.check("guards")
+
+
+def test_plans_on_two_streams_at_once():
+    """Two pools with workspaces of their own, on streams of their own: neither call sees the other's."""
+    print("case plans on two streams", flush=True)
+    rng = np.random.default_rng(77)
+    plans = []
+    for C in (300, 1300):
+        state = _state(rng, C, 500, 20, 5)
+        plans.append(Plan(*state, int(state[1].sum()) + 100))
+    torch.cuda.synchronize()
+    for p, stream in zip(plans, (torch.cuda.Stream(), torch.cuda.Stream())):
+        with torch.cuda.stream(stream):
+            p.call()
+    for i, p in enumerate(plans):
+        p.check(i)
+
+
 # -------------------------------------------------------------------------------------------------------- append
 
 class Cache:
@@ -255,6 +287,42 @@ def test_append_of_many_tokens(n_tokens, C, Hkv, D):
     cache = Cache(rng, int(pages.sum()), Hkv, D, "e4m3")
     cache.append(_rand(g, n_tokens, Hkv, D, scale=3), _rand(g, n_tokens, Hkv, D), slots)
     cache.check(n_tokens)
+
+
+def test_append_finds_few_slots_among_many_tokens():
+    """More tokens than one dimension of the launch holds workgroups for; slots in the first, the middle and the last of them."""
+    n = 32768 * 256 + 1000
+    print(f"case append few of {n}", flush=True)
+    rng = np.random.default_rng(5)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    cache = Cache(rng, 9, 1, 64, "e4m3")
+    k, v = _rand(g, n, 1, 64), _rand(g, n, 1, 64)
+    at = np.concatenate([np.arange(70), n // 2 + np.arange(130), n - 90 + np.arange(90)])
+    places = np.concatenate([7 * 64 + 5 + np.arange(59), 0 * 64 + np.arange(11), 3 * 64 + np.arange(64), 4 * 64 + np.arange(64), 2 * 64 + np.arange(2),
+                             5 * 64 + np.arange(64), 6 * 64 + np.arange(26)])
+    slots = np.full(n, -1, dtype=np.int64)
+    slots[at] = places
+    pe.peagle_cache_append_scaled(pe.CacheShape(n, 1, 64, 9), k, v, torch.from_numpy(slots).cuda(), *cache.pages, *cache.scales)
+    rows = torch.from_numpy(at).cuda()
+    for x, values, exps in zip((k, v), cache.values, cache.exps):
+        orc.cache_append(bf16_to_f64(x[rows]), places, values, exps, "e4m3")
+    cache.check("few of many")
+
+
+@pytest.mark.parametrize("Hkv,D,n_tokens", [(1, 64, 1), (3, 128, 77), (2, 64, 700)])
+def test_append_stays_inside_its_buffers(Hkv, D, n_tokens):
+    print(f"case append guards Hkv={Hkv} D={D}", flush=True)
+    rng = np.random.default_rng(n_tokens)
+    gen = torch.Generator(device="cuda").manual_seed(n_tokens)
+    cache = Cache(rng, -(-n_tokens // 64) + 1, Hkv, D, "e5m2")
+    g = Guarded()
+    cache.pages = [g.tensor(f"pages {i}", tuple(x.shape), x.dtype).copy_(x) for i, x in enumerate(cache.pages)]
+    cache.scales = [g.tensor(f"scales {i}", tuple(x.shape), torch.uint8).copy_(x.view(torch.uint8)).view(E8M0) for i, x in enumerate(cache.scales)]
+    last = cache.n_pages * 64
+    slots = np.arange(last - n_tokens, last)
+    cache.append(_rand(gen, n_tokens, Hkv, D, scale=50), _rand(gen, n_tokens, Hkv, D), slots)
+    g.check("append")
+    cache.check("guards")
 
 
 def test_append_skips_tokens_without_a_slot():

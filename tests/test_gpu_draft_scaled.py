@@ -156,6 +156,23 @@ def test_draft_scaled_batches_on_a_shared_pool(C, ctx, K, Hq, Hkv, D):
     assert np.array_equal(o2[others], o[others]) and np.array_equal(lse2[others], lse[others]) and np.isfinite(o2).all()
 
 
+@pytest.mark.parametrize("C,ctx,K,Hq,Hkv,D", [(70, 900, 7, 32, 4, 64), (130, 5000, 4, 64, 4, 64), (100, 2500, 7, 24, 4, 128), (40, 1500, 16, 64, 8, 64),
+                                              (40, 6000, 4, 256, 8, 64)])
+def test_draft_scaled_batches_in_e5m2(C, ctx, K, Hq, Hkv, D):
+    """More workgroups than compute units, by request and in shares: two to four blocks of rows."""
+    rng = np.random.default_rng(C + ctx)
+    lens = rng.integers(0, ctx, C)
+    lens[C // 3] = ctx
+    lens[C // 2] = 0
+    print(f"case scaled e5m2 batch C={C} ctx={ctx} D={D}", flush=True)
+    r = ScaledRun(tuple(int(x) for x in lens), K, Hq, Hkv, D, "e5m2", C, shared=50)
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    r.check(o, lse, "batch", (0, C // 3, C // 2, C - 1))
+    o2, lse2, _ = r.run()
+    assert np.array_equal(o, o2) and np.array_equal(lse, lse2)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_draft_scaled_flags_bad_tables_and_lengths(D):
     """Page ids on both sides of the pool, lengths below zero and beyond the table: flagged, skipped or clamped as the bf16
