@@ -616,7 +616,8 @@ def _stream_on(device: int, stream):
     import torch
     if device != torch.cuda.current_device():
         raise ValueError(f"the tensors live on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream_ptr(stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw and stream is None else _stream_ptr(stream)
 
 
 def peagle_cache_plan(shape: PlanShape, ctx_len, new_len, pages_held, free_pages, free_count, block_table, token_start, slots,
@@ -672,17 +673,14 @@ def _cache_pools(device, k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: 
             _ptr_on(device, k_scale, "k_scale", e8, scales), _ptr_on(device, v_scale, "v_scale", e8, scales))
 
 
-def _rows_ptr(device: int, t, name: str, shape):
-    """Device pointer and row distance (elements) of a bf16 tensor whose rows are whole but may stand apart."""
-    import torch
-    if t.dtype is not torch.bfloat16:
-        raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
+def _rows_ptr(device: int, t, name: str, dtype, shape):
+    """Device pointer and row distance (elements) of a tensor whose rows are whole but may stand apart."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must live on the GPU")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: lives on {t.device}, other tensors of the call on cuda:{device}")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name}: must live on the GPU, with the other tensors of the call; lives on {t.device}")
     n, H, D = shape
     along, across, inner = t.stride()
     if (D > 1 and inner != 1) or (H > 1 and across != D):
@@ -696,8 +694,8 @@ def peagle_cache_append_scaled(shape: CacheShape, k_new, v_new, slots, k_pages, 
     s, dev = shape, k_pages.get_device()
     fmt, *pools = _cache_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
     rows = (s.n_tokens, s.Hkv, s.D)
-    k, k_stride = _rows_ptr(dev, k_new, "k_new", rows)
-    v, v_stride = _rows_ptr(dev, v_new, "v_new", rows)
+    k, k_stride = _rows_ptr(dev, k_new, "k_new", torch.bfloat16, rows)
+    v, v_stride = _rows_ptr(dev, v_new, "v_new", torch.bfloat16, rows)
     at = _ptr_on(dev, slots, "slots", torch.int64, (s.n_tokens,))
     c = _CacheShapeC(s.n_tokens, s.Hkv, s.D, s.n_pages, fmt, k_stride, v_stride)
     rc = load_library().peagle_cache_append_scaled(C.byref(c), k, v, at, *pools, _stream_on(dev, stream))
