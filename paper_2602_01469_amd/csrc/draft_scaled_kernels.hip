@@ -613,46 +613,49 @@ __global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void
   }
 }
 
-// Merges a request's partial records: M = max m_s, each sum and O the sum of the records' times 2^(m_s - M).  A workgroup takes
-// kRows rows; a row's threads - D / 4 for its features, kLanes of them for the records in turn - look at kEach records at a time,
-// whose loads are issued before the first is used.
-template <int D>
+// Merges a request's partial records: M = max m_s, each sum and O the sum of the records' times 2^(m_s - M).  A row's threads - D / 4
+// for its features, LANES of them for the records in turn - look at EACH records at a time, whose loads are issued before the
+// first is used.
+template <int D, int LANES>
+constexpr int kMergeRows = 256 / (D / 4 * LANES);  // of a workgroup
+template <int D, int LANES, int EACH>
 __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeParams sp) {
-  constexpr int kLanes = 256 / D, kEach = 8;
   const DecodeParams& p = sp.d;
-  const int lane = threadIdx.x & 63, d4 = lane % (D / 4), sl = lane / (D / 4);
+  const int d4 = threadIdx.x % (D / 4), sl = threadIdx.x / (D / 4) % LANES;
   const int kvh = blockIdx.y, c = blockIdx.z, n_rows = p.K * p.group;
   const int2 piece = sp.pieces[c];
   const int n = piece.y;
   if (n <= 1) return;  // (its workgroup has left the results)
-  const int row = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
+  const int row = (int)blockIdx.x * kMergeRows<D, LANES> + (int)threadIdx.x / (D / 4 * LANES);
   if (row >= n_rows) return;
   // record 0 may be its workgroup's second, the others are their workgroups' first
   const size_t rec0 = (size_t)kvh * sp.shares * 2;
   auto record = [&](int s) { return rec0 + (s == 0 ? piece.x : (piece.x / 2 + s) * 2); };
   float M = -3.402823466e38f, L = 0.f, W = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  bool bad = false;
-  for (int s0 = 0; s0 < n; s0 += kLanes * kEach) {
-    f32x4 ml[kEach], ov[kEach];
+  int bad = 0;
+  for (int s0 = 0; s0 < n; s0 += LANES * EACH) {
+    f32x4 ml[EACH], ov[EACH];
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {  // (records past the last are read as the last)
-      const int s = s0 + j * kLanes + sl;
+    for (int j = 0; j < EACH; ++j) {
+      if (s0 + j * LANES >= n) continue;
+      const int s = s0 + j * LANES + sl;  // (past the last it is read again)
       const size_t at = record(s < n ? s : n - 1) * p.rows_pad + row;
       ml[j] = reinterpret_cast<const f32x4*>(p.part_ml)[at];
       ov[j] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + d4 * 4);
     }
     float m_new = M;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) m_new = __builtin_fmaxf(m_new, ml[j][0]);
+    for (int j = 0; j < EACH; ++j)
+      if (s0 + j * LANES < n) m_new = __builtin_fmaxf(m_new, ml[j][0]);
     const float turn = exp2_fast(M - m_new);
     M = m_new;
     L *= turn;
     W *= turn;
     acc *= turn;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (s0 + j * kLanes + sl < n) {  // (not by a weight of zero: a record may hold infinities)
+    for (int j = 0; j < EACH; ++j) {
+      if (s0 + j * LANES + sl < n) {  // (not by a weight of zero: a record may hold infinities)
         const float w = exp2_fast(ml[j][0] - M);
         L = __builtin_fmaf(ml[j][1], w, L);
         W = __builtin_fmaf(ml[j][2], w, W);
@@ -662,7 +665,7 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
     }
   }
 #pragma unroll
-  for (int x = D / 4; x < 64; x <<= 1) {
+  for (int x = D / 4; x < D / 4 * LANES; x <<= 1) {
     const float m_other = __shfl_xor(M, x), m_new = __builtin_fmaxf(M, m_other);
     const float a = exp2_fast(M - m_new), b = exp2_fast(m_other - m_new);
     M = m_new;
@@ -670,12 +673,10 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
     W = W * a + __shfl_xor(W, x) * b;
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + __shfl_xor(acc[j], x) * b;
-  }
-  if (p.status && row == 0 && kvh == 0) {
-    const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
-    if (lane == 0) p.status[c] = any;
+    bad |= __shfl_xor(bad, x);
   }
   if (sl != 0) return;
+  if (p.status && row == 0 && kvh == 0 && d4 == 0) p.status[c] = bad;
   const float inv = 1.0f / W;
   const int depth = small_quotient(row, p.group_reciprocal), head = kvh * p.group + (row - depth * p.group);
   u32x2 out;
@@ -753,9 +754,16 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, 
   e5m2 ? go(std::true_type{}) : go(std::false_type{});
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.shares == 0) return e;
-  const dim3 rows((unsigned)((p.d.K * p.d.group + 3) / 4), (unsigned)p.d.Hkv, (unsigned)p.d.C);
-  if (D == 64) hipLaunchKernelGGL(draft_scaled_combine_kernel<64>, rows, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL(draft_scaled_combine_kernel<128>, rows, dim3(256), 0, stream, p);
+  auto merge = [&](auto kernel, int rows) {
+    const dim3 grid((unsigned)((p.d.K * p.d.group + rows - 1) / rows), (unsigned)p.d.Hkv, (unsigned)p.d.C);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p);
+  };
+  // One thread for all of a row's records and four features where a request has a few records (64 requests of 512 to 8192 tokens, two or
+  // three each: the step 79.8 us, 83.2 with four), otherwise four (D 64; two at D 128), or each would wait for more reads one after the
+  // other (4 requests, nine each: 14.6, 15.1 with one).
+  const bool few = p.shares <= 4 * p.d.C;
+  if (D == 64) few ? merge(draft_scaled_combine_kernel<64, 1, 4>, kMergeRows<64, 1>) : merge(draft_scaled_combine_kernel<64, 4, 4>, kMergeRows<64, 4>);
+  else few ? merge(draft_scaled_combine_kernel<128, 1, 4>, kMergeRows<128, 1>) : merge(draft_scaled_combine_kernel<128, 2, 8>, kMergeRows<128, 2>);
   return hipGetLastError();
 }
 
