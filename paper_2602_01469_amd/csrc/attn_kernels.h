@@ -134,6 +134,7 @@ struct ShareRule {
   int shares;  // workgroups that share the work of a KV head (0: one for each request)
   int least;   // units that a workgroup takes at least
   int lead;    // units that the start of a request counts for
+  int waves;   // of a workgroup
 };
 ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D);  // blocks: of 32 query rows
 

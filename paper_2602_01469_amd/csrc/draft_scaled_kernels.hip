@@ -292,15 +292,17 @@ __device__ __forceinline__ T* held(T* x) {  // (as a pointer to global memory, w
 
 // Workgroup = (share of the work, KV head).  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that share the KV head (row =
 // depth * group + head); PARTS waves with different rows make a stream, and the streams take a request's pages in turn.  A stream
-// has a ring of slots in LDS (32 tokens each), filled by its waves some slots ahead of their use.  With one wave a stream (up to
-// 32 rows, at D = 64 up to 64) a wave waits for its own copies only and the loop has no barrier; more rows share what a stream
-// copies, which costs a barrier a slot.  At the end of a request's pages the streams' sums are merged through LDS, and leave the
-// results where the request is one workgroup's, otherwise a partial record.
-template <int D, int RB>
-constexpr int kWavesOf = D == 64 && RB == 1 ? 8 : 4;  // of a workgroup, two workgroups a CU: 128 KiB of rings
-template <int D, bool E5M2, int RB, int PARTS>
-__global__ __launch_bounds__((kWavesOf<D, RB>) * 64, (kWavesOf<D, RB>) / 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
-  constexpr int kWaves = kWavesOf<D, RB>, kStreams = kWaves / PARTS, kRing = 65536 / kStreams;  // waves, streams, bytes of a ring
+// has a ring of slots in LDS (a page each where the ring holds two, otherwise 32 tokens), filled by its waves some slots ahead of their
+// use.  With one wave a stream (up to 32 rows, at D = 64 up to 64) a wave waits for its own copies only and the loop has no barrier;
+// more rows share what a stream copies, which costs a barrier a slot.  At the end of a request's pages the streams' sums are merged
+// through LDS, and leave the results where the request is one workgroup's, otherwise a partial record.
+// Bound: memory (64 requests of 8192 tokens: 102 us on MI355X with 24 rows of 128 features, 5.3 TB/s), with 56 rows of 64 features
+// vector issue beside it (121 us, 4.4 TB/s: 204 instructions a slot of 32 keys and 64 rows - a quarter of it exponentials - keep the vector
+// units busy for 64 % of a wave's time, the 16 matrix instructions theirs for 34 %).
+template <int D, bool E5M2, int RB, int PARTS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
+  constexpr int kWaves = WAVES, kStreams = kWaves / PARTS;
+  constexpr int kRing = (D == 64 && RB == 1 ? 8192 : 16384) * kWaves / kStreams;  // bytes of a stream's ring: 128 KiB a CU
   constexpr int kTokens = kRing >= 4 * 64 * D ? 64 : 32, kHalf = kTokens * D, kSlot = 2 * kHalf;  // a slot: bytes of its keys, in all
   constexpr int kPerPage = kKeysPerTile / kTokens, kDepth = kRing / kSlot;                        // slots of a page, of a ring
   constexpr int kCopies = kSlot / 1024 / PARTS;                               // of a slot, by each of a stream's waves
@@ -687,11 +689,6 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
 }
 
 constexpr int kCus = 256;  // compute units of the device
-// Streams of a workgroup for rows in `blocks` of 32.
-int streams_of(int D, int blocks) {
-  if (D == 64) return blocks == 1 ? 8 : blocks == 2 ? 4 : 2;
-  return blocks == 1 ? 4 : blocks == 2 ? 2 : 1;
-}
 
 }  // namespace
 
@@ -706,19 +703,34 @@ int streams_of(int D, int blocks) {
 //          of 768 tokens: 14.1 against 15.8).
 //   shares a workgroup on each CU while each would have fewer than 12 units with two a CU, as the starts and the records weigh
 //          more than the reads in flight: 16.1 against 18.8 for 4 requests of 2048 to 4096, 21.9 against 25.9 for 2 of 10800 to
-//          20000 (D 128), 17.5 against 20.3 for one of 20000.  Above that two: 89.7 against 95.6 for 64 of 512 to 8192, 101
-//          against 117 for 48 of 500 to 8191 (D 128, 128 rows).
+//          20000 (D 128), 17.5 against 20.3 for one of 20000.  Above that D 64 takes two a CU: 89.7 against 95.6 for 64 of 512 to
+//          8192.
+//   waves  D 128 takes one workgroup of eight waves a CU there instead, which leaves half the records: 48 of 500 to 8191 (128
+//          rows) 91 against 95, 64 of 8192 (24 rows) 102 against 116.  (D 64: 84 against 80, by request too, as its starts find no other
+//          workgroup to work meanwhile.)  By request likewise where a CU gets one workgroup anyway: 40 of 300 to 2000 with 24 rows 16.7
+//          against 18.7, with 128 rows 27.5 against 26.9; with several for each CU two side by side are better: 100 of 100 to 1000
+//          with 128 rows 27.9 against 33.9.
 ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
-  const int streams = streams_of(D, blocks);
   ShareRule r;
+  r.waves = D == 64 && blocks == 1 ? 8 : 4;
+  // Streams that these waves make: a block of rows, at D = 64 two, is a wave's.
+  int streams = r.waves / (D == 64 ? (blocks + 1) / 2 : blocks == 3 ? 4 : blocks);
   r.least = 2 * streams;
   r.lead = 8;
   r.shares = 0;
   const int64_t most = (int64_t)C * (max_pages + r.lead + 1);  // units of a KV head
   if (C > 1024 || max_pages <= 2 * streams || most > INT_MAX) return r;
-  if (max_pages <= 8 * streams && (int64_t)C * Hkv >= kCus / 2) return r;
-  const int per_cu = most * Hkv >= 12 * 2 * kCus ? 2 : 1;
-  const int64_t slots = (per_cu * kCus + Hkv - 1) / Hkv, useful = (most + r.least - 1) / r.least;
+  if (max_pages <= 8 * streams && (int64_t)C * Hkv >= kCus / 2) {
+    if (D == 128 && (int64_t)C * Hkv <= kCus) r.waves = 8;
+    return r;
+  }
+  const bool large = most * Hkv >= 12 * 2 * kCus;
+  if (D == 128 && large) {
+    r.waves = 8;
+    r.least *= 2;
+  }
+  const int64_t wgs = large && D == 64 ? 2 * kCus : kCus;
+  const int64_t slots = (wgs + Hkv - 1) / Hkv, useful = (most + r.least - 1) / r.least;
   r.shares = (int)(slots < useful ? slots : useful);
   return r;
 }
@@ -741,14 +753,18 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, 
     constexpr bool T = decltype(type)::value;
     auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)waves * 64), 0, stream, p); };
     if (D == 64) {
-      if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1>, kWavesOf<64, 1>);
-      else if (blocks == 2 && alone) run(draft_scaled_kernel<64, T, 1, 2>, kWavesOf<64, 1>);
-      else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1>, kWavesOf<64, 2>);
-      else run(draft_scaled_kernel<64, T, 2, 2>, kWavesOf<64, 2>);
+      if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1, 8>, 8);
+      else if (blocks == 2 && alone) run(draft_scaled_kernel<64, T, 1, 2, 8>, 8);
+      else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1, 4>, 4);
+      else run(draft_scaled_kernel<64, T, 2, 2, 4>, 4);
+    } else if (rule.waves == 4) {
+      if (blocks == 1) run(draft_scaled_kernel<128, T, 1, 1, 4>, 4);
+      else if (blocks == 2) run(draft_scaled_kernel<128, T, 1, 2, 4>, 4);
+      else run(draft_scaled_kernel<128, T, 1, 4, 4>, 4);
     } else {
-      if (blocks == 1) run(draft_scaled_kernel<128, T, 1, 1>, kWavesOf<128, 1>);
-      else if (blocks == 2) run(draft_scaled_kernel<128, T, 1, 2>, kWavesOf<128, 1>);
-      else run(draft_scaled_kernel<128, T, 1, 4>, kWavesOf<128, 1>);
+      if (blocks == 1) run(draft_scaled_kernel<128, T, 1, 1, 8>, 8);
+      else if (blocks == 2) run(draft_scaled_kernel<128, T, 1, 2, 8>, 8);
+      else run(draft_scaled_kernel<128, T, 1, 4, 8>, 8);
     }
   };
   e5m2 ? go(std::true_type{}) : go(std::false_type{});
@@ -762,8 +778,8 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, 
   // three each: the step 79.8 us, 83.2 with four), otherwise four (D 64; two at D 128), or each would wait for more reads one after the
   // other (4 requests, nine each: 14.6, 15.1 with one).
   const bool few = p.shares <= 4 * p.d.C;
-  if (D == 64) few ? merge(draft_scaled_combine_kernel<64, 1, 4>, kMergeRows<64, 1>) : merge(draft_scaled_combine_kernel<64, 4, 4>, kMergeRows<64, 4>);
-  else few ? merge(draft_scaled_combine_kernel<128, 1, 4>, kMergeRows<128, 1>) : merge(draft_scaled_combine_kernel<128, 2, 8>, kMergeRows<128, 2>);
+  if (D == 64) few ? merge(draft_scaled_combine_kernel<64, 1, 4>, kMergeRows<64, 1>) : merge(draft_scaled_combine_kernel<64, 4, 8>, kMergeRows<64, 4>);
+  else few ? merge(draft_scaled_combine_kernel<128, 1, 4>, kMergeRows<128, 1>) : merge(draft_scaled_combine_kernel<128, 2, 16>, kMergeRows<128, 2>);
   return hipGetLastError();
 }
 

@@ -157,7 +157,8 @@ def test_draft_scaled_batches_on_a_shared_pool(C, ctx, K, Hq, Hkv, D):
 
 
 @pytest.mark.parametrize("C,ctx,K,Hq,Hkv,D", [(70, 900, 7, 32, 4, 64), (130, 5000, 4, 64, 4, 64), (100, 2500, 7, 24, 4, 128), (40, 1500, 16, 64, 8, 64),
-                                              (40, 6000, 4, 256, 8, 64)])
+                                              (40, 6000, 4, 256, 8, 64), (64, 5000, 3, 16, 8, 128), (64, 4000, 8, 64, 4, 128), (40, 1500, 3, 32, 4, 128),
+                                              (50, 2000, 7, 32, 4, 128), (33, 1900, 16, 32, 4, 128)])
 def test_draft_scaled_batches_in_e5m2(C, ctx, K, Hq, Hkv, D):
     """More workgroups than compute units, by request and in shares: two to four blocks of rows."""
     rng = np.random.default_rng(C + ctx)
