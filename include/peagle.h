@@ -426,13 +426,13 @@ int peagle_draft_decode_static(const peagle_decode_shape_t* shape, const void* q
  *   status       device, int32 [C] (out): 0 served; 1 a length is negative, the sum beyond the table, pages_held outside
  *                [ceil(ctx_len / 64), max_pages] or the last new row beyond max_tokens; 2 no pages left.  Such a request
  *                keeps what it holds; its rows (none for a negative new_len) count in token_start and get slots of -1
- *   workspace    device, >= peagle_cache_plan_workspace_bytes(); contents undefined before and after
+ *   workspace    device, 16-byte aligned, >= peagle_cache_plan_workspace_bytes(); contents undefined before and after
  *
  * Pages are given back before any are taken, those of the last request first and of each request the last block first, so
  * that what ends in one call stands on the list as it did before it was taken in one.  They are taken in order of the requests
  * and blocks; the first request that does not find all it lacks and those after it that lack any get none.  A free_count
  * outside [0, n_pages] is clamped; page ids outside the pools are passed on to the table, with slots of -1.  Entries of
- * free_pages at and behind free_count_out are left as they are.
+ * free_pages at and behind free_count_out hold pages that were there once and mean nothing.
  */
 typedef struct peagle_plan_shape {
   int32_t C, max_pages, n_pages, max_tokens;
@@ -453,7 +453,8 @@ int peagle_cache_plan(const peagle_plan_shape_t* shape, const int32_t* ctx_len, 
  *   slots        device, int64 [n_tokens]: 64 * page + place in the page; a token whose slot is outside [0, 64 * n_pages)
  *                is not stored
  *   k_pages, v_pages   device, 8-bit [n_pages, Hkv, 64, D] (in and out), 16-byte aligned
- *   k_scale, v_scale   device, uint8 [n_pages, Hkv] (in and out)
+ *   k_scale, v_scale   device, uint8 [n_pages, Hkv] (in and out); no call leaves a code above 247, and where a run goes on
+ *                behind one of 254 or 255 from elsewhere, zeros are stored
  *
  * Consecutive rows with consecutive slots of one page are a run.  A run that begins at place 0 begins the page: its scale is
  * the smallest power of two, at least 2^-100, that brings the run's largest finite value to the type's largest (448 or 57344)
@@ -473,10 +474,11 @@ int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, const void* k_
                                void* k_pages, void* v_pages, void* k_scale, void* v_scale, void* stream);
 
 /*
- * peagle_draft_decode on such a cache: the same shape, arguments and results, with 8-bit pools (16-byte aligned) of the type
- * `format` and their scales k_scale, v_scale (device, uint8 [n_pages, Hkv]; any code, 255 is NaN).  The new positions' keys
- * and values are bf16, as there.  Codes and scales become bf16 without rounding; scores, row sums and outputs are summed in
- * fp32, probabilities are rounded to bf16 before they weigh the values.
+ * peagle_draft_decode on such a cache: the same shape, arguments and results, with 8-bit pools of the type `format` and
+ * their scales k_scale, v_scale (device, uint8 [n_pages, Hkv]; any code, 255 is NaN).  The pools, q_new, k_new, v_new, o and
+ * the workspace are 16-byte aligned.  The new positions' keys and values are bf16, as there.  Codes and scales become bf16
+ * without rounding; scores, row sums and outputs are summed in fp32, probabilities are rounded to bf16 before they weigh
+ * the values.
  */
 size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode_shape_t* shape);
 int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,

@@ -712,6 +712,7 @@ extern "C" int peagle_cache_plan(const peagle_plan_shape_t* shape, const int32_t
       !token_start || !slots || !seq_len || !status)
     return PEAGLE_ENULL;
   if (!workspace || ws_bytes < peagle_cache_plan_workspace_bytes(shape)) return PEAGLE_EWORKSPACE;
+  if (!aligned16(workspace)) return PEAGLE_EINVAL;
   peagle::PlanParams p{};
   p.ctx_len = ctx_len;
   p.new_len = new_len;
@@ -804,6 +805,7 @@ extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, in
     return PEAGLE_EINVAL;
   const ScaledWs w = decode_scaled_ws(shape);
   if (!workspace || ws_bytes < w.total) return PEAGLE_EWORKSPACE;
+  if (!aligned16(workspace)) return PEAGLE_EINVAL;
   peagle::ScaledDecodeParams p{};
   p.pieces = (int2*)((char*)workspace + w.pieces_off);
   p.d = decode_params(shape, w.records, q_new, k_new, v_new, block_table, ctx_len, o, lse, status, workspace);

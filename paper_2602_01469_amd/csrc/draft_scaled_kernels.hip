@@ -719,7 +719,7 @@ ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
   r.lead = 8;
   r.shares = 0;
   const int64_t most = (int64_t)C * (max_pages + r.lead + 1);  // units of a KV head
-  if (C > 1024 || max_pages <= 2 * streams || most > INT_MAX) return r;
+  if (C > 1024 || max_pages <= 2 * streams || most > 1 << 30) return r;
   if (max_pages <= 8 * streams && (int64_t)C * Hkv >= kCus / 2) {
     if (D == 128 && (int64_t)C * Hkv <= kCus) r.waves = 8;
     return r;

@@ -91,6 +91,7 @@ def test_plan_refuses_missing_arguments_and_short_workspaces():
         assert _plan_call((4, 4, 8, 8), **{n: None}) == ENULL, n
     assert _plan_call((4, 4, 8, 8), workspace=None) == EWORKSPACE
     assert _plan_call((20, 4, 8, 8), ws_bytes=255) == EWORKSPACE
+    assert _plan_call((4, 4, 8, 8), workspace=C.c_void_p(264)) == EINVAL
     assert pe.peagle_cache_plan_workspace_bytes(pe.PlanShape(20, 4, 8, 8)) == 512
 
 
@@ -163,6 +164,6 @@ def test_scaled_draft_refuses_formats_pointers_and_workspaces():
     assert _draft_call(format_=2) == EUNSUPPORTED and _draft_call(format_=-1) == EUNSUPPORTED
     for n in ("q_new", "k_new", "v_new", "k_pages", "v_pages", "k_scale", "v_scale", "block_table", "ctx_len", "o", "lse"):
         assert _draft_call(**{n: None}) == ENULL, n
-    for n in ("q_new", "k_new", "v_new", "k_pages", "v_pages", "o"):
+    for n in ("q_new", "k_new", "v_new", "k_pages", "v_pages", "o", "workspace"):
         assert _draft_call(**{n: C.c_void_p(264)}) == EINVAL, n
     assert _draft_call(workspace=None) == EWORKSPACE and _draft_call(ws_bytes=16) == EWORKSPACE
