@@ -694,7 +694,8 @@ constexpr int kCus = 256;  // compute units of the device
 
 // How the work of a KV head is shared, from the sizes that the host knows; times as microseconds a step on MI355X, D 64, 8 heads
 // of keys, 7 or 8 rows a position unless noted.
-//   lead   the start of a share (its part of the lookup, queries, merge) takes as long as some 8 pages.
+//   lead   the start of a request's part (table, queries, merge) takes as long as some 8 pages: with 4 or 16 4 requests of 2048 to
+//          4096 take 16.6 or 15.3 instead of 14.7, 48 of 500 to 8191 (D 128, 128 rows) 95.8 or 96.3 instead of 91.
 //   least  two pages a stream, so that each wave has copies under way while it works.
 //   By request, without the second launch: where one request's pages are too few to divide (at most two a stream), and where
 //          eight a stream or fewer meet half the CUs' worth of workgroups: 14.8 against 21.1 for 16 requests of 1000 tokens, 22.0
