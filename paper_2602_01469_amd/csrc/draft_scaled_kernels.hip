@@ -107,6 +107,9 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
     for (int db = 0; db < D / 32; ++db)
       vw[t][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(PEAGLE_LDS_PTR(i32x2, v_at + v_off[db] + t * 16 * D));
   __builtin_amdgcn_sched_barrier(0);
+  // (A wave at its products goes before one at its softmax, which then has the vector units while the products run: 48 requests of
+  // 500 to 8191 tokens with 128 rows of 128 features 92.9 -> 87.9 us, 56 rows of 64 features 0 to 3 %.)
+  __builtin_amdgcn_s_setprio(1);
   f32x16 s[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
@@ -119,6 +122,7 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
       s[rb] = mfma32(a1, r.q[rb][2 * i + 1], s[rb]);
     }
   }
+  __builtin_amdgcn_s_setprio(0);
   if (n < 32) {
     const uint32_t bits = ((1u << n) - 1) >> (4 * g);
 #pragma unroll
@@ -129,6 +133,7 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
   bf16x8 pb[RB][2];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) soft(r, rb, s[rb], c, pb[rb]);
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -137,6 +142,7 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(a, pb[rb][t], r.o[rb][db]);
     }
+  __builtin_amdgcn_s_setprio(0);
 }
 
 // Sixteen of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
