@@ -91,7 +91,11 @@ __device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, const f32x16& s, fl
   pb[1] = pack8_sum(x, 1, r.w[rb]);
 }
 
-// 32 keys, staged with their values, of which the first n count (the others are masked; their values are finite).
+// The bytes of a word whose bits, from the lowest on, are set in `keep` (four of them).
+__device__ __forceinline__ uint32_t bytes_of(uint32_t keep) { return ((keep & 0xfu) * 0x00204081u & 0x01010101u) * 0xffu; }
+
+// 32 keys, staged with their values, of which the first n count.  The others are masked, and their codes of values made zero: a
+// probability of zero times an infinity, which E5M2 holds and any code becomes beyond bf16, would be NaN.
 template <int D, bool E5M2, int RB>
 __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, const int (&k_off)[D / 32],
                                             const int (&v_off)[D / 32], float ks, float vs, int n, int g, float c) {
@@ -129,6 +133,12 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) vw[t][db][w] &= (int)bytes_of(bits >> (16 * t + 8 * w));
   }
   bf16x8 pb[RB][2];
 #pragma unroll
@@ -448,7 +458,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         each_copy([&](bool half, int b) {
           dma16_untracked(uniform_ptr((half ? v_pages : k_pages) + at) + b * 1024, voff[b & 1], dst + (half ? kHalf : 0) + b * 1024);
         });
-      } else {  // rows behind the last token are read as that token: they are masked, and zero times its values adds nothing
+      } else {  // rows behind the last token are read as that token, and masked
         const int last = present > 0 ? present - 1 : 0, l = lane_id();
         each_copy([&](bool half, int b) {
           const int row = b * (64 / kLanes) + l / kLanes;

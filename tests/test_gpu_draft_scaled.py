@@ -401,3 +401,43 @@ def test_plan_append_and_draft_as_a_serving_loop_runs_them():
             got, got_lse = bf16_to_f64(o[c]), lse[c].double().cpu().numpy()
             assert rel_l2(got, ro) <= REL and max_abs(got_lse, rl) <= 8 * LSE_ABS, (step, c)
             assert rel_l2(held_v, kept[1][c]) <= 2.0**-4 and rel_l2(held_k, kept[0][c]) <= 2.0**-4
+
+
+ROWS = [(1, 2, 2), (7, 16, 2), (6, 32, 2), (8, 16, 1)]  # K, Hq, Hkv: one to four blocks of rows
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("K,Hq,Hkv", ROWS)
+def test_draft_scaled_shows_infinities_of_the_last_cached_token(K, Hq, Hkv, D):
+    """An infinity of E5M2 in V of the last cached token reaches that feature's outputs as an infinity of its sign, whether the
+    places behind the token are masked (lengths off a multiple of 32) or not; every other feature stays as the oracle has it."""
+    print(f"case scaled last token infinite K={K} Hq={Hq} D={D}", flush=True)
+    r = ScaledRun((64, 65, 95, 96, 97, 127, 1, 31, 33, 1000), K, Hq, Hkv, D, "e5m2", 4000 + K)
+    for c, n in enumerate(r.lens):
+        raw, page, at = r.pages[1].view(torch.uint8), int(r.table[c, (n - 1) // 64]), (n - 1) % 64
+        raw[page, 0, at, 5], raw[page, Hkv - 1, at, D - 1] = 0x7C, 0xFC
+    o, lse, status = r.run()
+    assert (status == 0).all() and np.isfinite(lse).all()
+    group = Hq // Hkv
+    for c in range(len(r.lens)):
+        ro, rl = r.oracle(c)
+        assert np.isposinf(ro[:, :group, 5]).all() and np.isneginf(ro[:, -group:, D - 1]).all()
+        finite = np.isfinite(ro)
+        assert np.array_equal(o[c][~finite], ro[~finite]), (c, r.lens[c])
+        assert rel_l2(o[c][finite], ro[finite]) <= REL and max_abs(lse[c], rl) <= LSE_ABS, (c, r.lens[c])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_draft_scaled_masks_codes_that_widen_to_infinity(D):
+    """A code and scale beyond bf16 in the last cached token: infinite in its own feature, and nowhere else."""
+    print(f"case scaled widened infinity D={D}", flush=True)
+    r = ScaledRun((65, 97, 64), 3, 8, 2, D, "e4m3", 4100)
+    for c, n in enumerate(r.lens):
+        page, at = int(r.table[c, (n - 1) // 64]), (n - 1) % 64
+        raw = r.pages[1].view(torch.uint8)
+        raw[page, :, :at + 1] = 0
+        raw[page, :, at, 5] = 0x7E                    # 448 * 2^127
+        r.scales[1].view(torch.uint8)[page] = 254
+    o, lse, status = r.run()
+    assert (status == 0).all() and np.isfinite(lse).all()
+    assert np.isposinf(o[..., 5]).all() and np.isfinite(np.delete(o, 5, 3)).all()
