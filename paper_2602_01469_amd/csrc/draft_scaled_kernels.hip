@@ -57,11 +57,15 @@ struct Rows {
 
 // Scores of 32 keys (registers <-> keys 8 (i / 4) + 4 g + i % 4) to probabilities, as operands of the product with the values.
 // A probability is rounded to bf16 to weigh its value, by up to 2^-9 of itself wherever it stands, so that the reference need not be
-// near the row's largest score.  It must not be far below it: it moves where a lane's sum of probabilities says so (also at the first
-// keys, which meet the start value), and no maximum is taken otherwise.  The output is divided by the sum of the rounded
+// near the row's largest score.  It must not be far below it: it moves where a lane's sum of probabilities is above `limit` (also at
+// the first keys, which meet the start value), and no maximum is taken otherwise.  The output is divided by the sum of the rounded
 // probabilities, which makes a row of one heavy key exact; the LSE takes the sum of the unrounded ones.
+// The limit keeps what is summed for the values inside fp32: with scales up to 2^40 a value is below 2^56, and weights of 2^41 a
+// block of 32 keys, up to 2^25 of them, leave their sum below 2^122.  Larger values are weighed by 1 at most, as by a running maximum.
+constexpr float kFarLimit = 0x1p40f, kNearLimit = 1.0f;
+constexpr int kFarScale = 127 + 40;  // largest code of a page's values that goes with kFarLimit
 template <int D, int RB>
-__device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, const f32x16& s, float c, bf16x8 (&pb)[2]) {
+__device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, const f32x16& s, float c, float limit, bf16x8 (&pb)[2]) {
   f32x16 x;
   auto weigh = [&] {
     float sum[4];
@@ -73,9 +77,9 @@ __device__ __forceinline__ void soft(Rows<D, RB>& r, int rb, const f32x16& s, fl
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
   float sum = weigh();
-  if (__builtin_amdgcn_ballot_w64(sum > 0x1p40f) != 0) {
+  if (__builtin_amdgcn_ballot_w64(sum > limit) != 0) {
     const float mx = max_halves(max16(s)) * c;
-    const bool need = max_halves(sum) > 0x1p40f && mx > r.m[rb];
+    const bool need = max_halves(sum) > limit && mx > r.m[rb];
     const float m_new = need ? mx : r.m[rb], alpha = exp2_fast(r.m[rb] - m_new);
     r.m[rb] = m_new;
     r.l[rb] *= alpha;
@@ -98,7 +102,8 @@ __device__ __forceinline__ uint32_t bytes_of(uint32_t keep) { return ((keep & 0x
 // probability of zero times an infinity, which E5M2 holds and any code becomes beyond bf16, would be NaN.
 template <int D, bool E5M2, int RB>
 __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, const int (&k_off)[D / 32],
-                                            const int (&v_off)[D / 32], float ks, float vs, int n, int g, float c) {
+                                            const int (&v_off)[D / 32], float ks, float vs, float limit, int n, int g,
+                                            float c) {
   // All LDS reads first: one at a time in front of its use, as the compiler places them otherwise, each would be waited for.
   typedef __attribute__((ext_vector_type(2))) int i32x2;
   u32x4 kw[D / 32];
@@ -142,7 +147,7 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
   }
   bf16x8 pb[RB][2];
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) soft(r, rb, s[rb], c, pb[rb]);
+  for (int rb = 0; rb < RB; ++rb) soft(r, rb, s[rb], c, limit, pb[rb]);
   __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
@@ -185,7 +190,7 @@ __device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* k_at, const
     const uint32_t bits = (n <= 0 ? 0u : (1u << n) - 1) >> (4 * g);
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
-    soft(r, rb, s[rb], c, pb[rb]);
+    soft(r, rb, s[rb], c, kNearLimit, pb[rb]);
   }
   bool odd = false;
 #pragma unroll
@@ -529,9 +534,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         if (starts) begin(q);
         const int j = i / 2, n = __builtin_amdgcn_readlane(keys, j) - i % 2 * 32;  // (0 behind this stream's pages)
         const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
-        const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(vcode, j) << 23);
+        const int v_code = __builtin_amdgcn_readlane(vcode, j);
+        const float vs = __builtin_bit_cast(float, v_code << 23), limit = v_code > kFarScale ? kNearLimit : kFarLimit;
         const char* at = ring[stream][q & (kDepth - 1)] + (kTokens == 32 ? 0 : i % 2 * 32 * D);
-        if (n > 0) cached_keys<D, E5M2, RB>(r, at, at + kHalf, k_off, v_off, ks, vs, n, g, p.c_log2);
+        if (n > 0) cached_keys<D, E5M2, RB>(r, at, at + kHalf, k_off, v_off, ks, vs, limit, n, g, p.c_log2);
         if (ends) {
           end();
           ++q;

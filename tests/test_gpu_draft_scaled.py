@@ -441,3 +441,49 @@ def test_draft_scaled_masks_codes_that_widen_to_infinity(D):
     o, lse, status = r.run()
     assert (status == 0).all() and np.isfinite(lse).all()
     assert np.isposinf(o[..., 5]).all() and np.isfinite(np.delete(o, 5, 3)).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("K,Hq,Hkv", ROWS)
+def test_draft_scaled_large_values_under_keys_that_stand_out(K, Hq, Hkv, D, fmt):
+    """Values up to 2^101 whose keys score 28 or 32 powers of two above those before them: outputs are their weighted means, far
+    from what fp32 holds at most, and so must be what is summed for them.  Some pages' values are small, on either side of them."""
+    print(f"case scaled large values K={K} Hq={Hq} D={D} {fmt}", flush=True)
+    r = ScaledRun((64 * 30, 100, 64 * 3 + 50), K, Hq, Hkv, D, fmt, 4200 + K, scale=float(np.log(2)), spare=0)
+    keys = torch.zeros(r.pages[0].shape)
+    keys[0::2, :, 40, 0], keys[1::2, :, 40, 0] = 28.0, 32.0
+    r.pages[0].copy_(keys.to(TYPES[fmt]).cuda())
+    r.scales[0].view(torch.uint8).fill_(127)
+    top = 101 - (9 if fmt == "e4m3" else 16)
+    r.scales[1].view(torch.uint8).copy_(torch.where(torch.arange(r.shape.n_pages) % 3 == 0, 120, 127 + top)[:, None].to(torch.uint8).cuda())
+    q, k, _ = (bf16_bits_to_f64(x).astype(np.float32) for x in r.host)
+    q[..., 0] = 1.0
+    r.host[0], r.host[1] = f32_to_bf16_bits(q), f32_to_bf16_bits(np.zeros_like(k))
+    r.q, r.k = to_dev_bf16(r.host[0]), to_dev_bf16(r.host[1])
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    for c in range(len(r.lens)):
+        ro, rl = r.oracle(c)
+        assert np.isfinite(o[c]).all() and (c != 0 or np.abs(ro).max() > 2.0**90), c
+        assert rel_l2(o[c], ro) <= REL and max_abs(lse[c], rl) <= LSE_ABS, (c, rel_l2(o[c], ro))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_draft_scaled_large_new_values_under_keys_that_stand_out(D):
+    """The same of new keys beyond the first sixteen."""
+    print(f"case scaled large new values D={D}", flush=True)
+    r = ScaledRun((0, 40), 40, 4, 2, D, "e4m3", 4300, scale=float(np.log(2)), spare=0)
+    r.pages[0].view(torch.uint8).zero_()
+    q, k, v = (bf16_bits_to_f64(x).astype(np.float32) for x in r.host)
+    q[..., 0] = 1.0
+    k[:] = 0.0
+    k[:, 20, :, 0], k[:, 33, :, 0] = 28.0, 32.0
+    v *= 2.0**100
+    r.host = [f32_to_bf16_bits(x) for x in (q, k, v)]
+    r.q, r.k, r.v = (to_dev_bf16(x) for x in r.host)
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    for c in range(2):
+        ro, rl = r.oracle(c)
+        assert np.isfinite(o[c]).all() and rel_l2(o[c], ro) <= REL and max_abs(lse[c], rl) <= LSE_ABS, c
