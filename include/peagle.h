@@ -453,8 +453,8 @@ int peagle_cache_plan(const peagle_plan_shape_t* shape, const int32_t* ctx_len, 
  *   slots        device, int64 [n_tokens]: 64 * page + place in the page; a token whose slot is outside [0, 64 * n_pages)
  *                is not stored
  *   k_pages, v_pages   device, 8-bit [n_pages, Hkv, 64, D] (in and out), 16-byte aligned
- *   k_scale, v_scale   device, uint8 [n_pages, Hkv] (in and out); no call leaves a code above 247, and where a run goes on
- *                behind one of 254 or 255 from elsewhere, zeros are stored
+ *   k_scale, v_scale   device, uint8 [n_pages, Hkv] (in and out); no call makes a code above 247.  A run that goes on behind a
+ *                larger one from elsewhere leaves it; behind 254 or 255 its finite values are stored as zeros, others as NaN
  *
  * Consecutive rows with consecutive slots of one page are a run.  A run that begins at place 0 begins the page: its scale is
  * the smallest power of two, at least 2^-100, that brings the run's largest finite value to the type's largest (448 or 57344)
@@ -477,8 +477,10 @@ int peagle_cache_append_scaled(const peagle_cache_shape_t* shape, const void* k_
  * peagle_draft_decode on such a cache: the same shape, arguments and results, with 8-bit pools of the type `format` and
  * their scales k_scale, v_scale (device, uint8 [n_pages, Hkv]; any code, 255 is NaN).  The pools, q_new, k_new, v_new, o and
  * the workspace are 16-byte aligned.  The new positions' keys and values are bf16, as there.  Codes and scales become bf16
- * without rounding; scores, row sums and outputs are summed in fp32, probabilities are rounded to bf16 before they weigh
- * the values.
+ * without rounding where the product is a normal bf16 number, as it is for all codes of E4M3 with scale codes 10 to 246 and of
+ * E5M2 with 17 to 239.  Smaller products are zero; those from 2^128 on are infinite, which an append makes of the largest
+ * bf16 values only (from 1.9375 * 2^127 on in E4M3, 1.875 * 2^127 in E5M2: 2^128 is their nearest code).  Scores, row sums and
+ * outputs are summed in fp32; probabilities are rounded to bf16 before they weigh the values.
  */
 size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode_shape_t* shape);
 int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,

@@ -2,10 +2,10 @@
 // each page and KV head: the K new rows of each request see its cached keys and the new keys of their own chain.
 //
 // With k = 2^ek a and v = 2^ev b for the codes a, b of a page, S = scale Q K^T, P = 2^(S log2(e) - m), O = P V / sum P.  A code
-// has four significant bits or three, so that with its page's scale it is a bf16 number: codes are widened to bf16, scale and all, by
-// one instruction for two of them, between LDS and the matrix instruction.  (The matrix instruction for 8-bit types, with queries
-// split into two numbers of them, would need no widening of keys, but its sums are not fp32 sums: 64 products of normal data came
-// out 4e-5 of the largest sum off.)
+// has four significant bits or three, so that with its page's scale it is a bf16 number (zero where that would not be a normal one,
+// infinite from 2^128 on): codes are widened to bf16, scale and all, by one instruction for two of them, between LDS and the
+// matrix instruction.  (The matrix instruction for 8-bit types, with queries split into two numbers of them, would need no widening
+// of keys, but its sums are not fp32 sums: 64 products of normal data came out 4e-5 of the largest sum off.)
 // The cache is read once, 2 Hkv D bytes a token, and bounds a large call; a small one is a chain of memory round trips.
 #include "attn_kernels.h"
 #include "attn_util.h"

@@ -380,6 +380,26 @@ def test_append_of_values_at_the_edges(fmt):
         cache.check(("added", step))
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_append_behind_the_largest_scales(fmt):
+    """Pages from elsewhere whose scales are above what an append makes: kept, with the new values rounded to them; behind the codes
+    254 and 255 finite values become zeros and others NaN."""
+    print(f"case append large scales {fmt}", flush=True)
+    rng, big = np.random.default_rng(14), 3.3895313892515355e38
+    x = torch.tensor([big, -big, 1.5 * 2.0**120, 2.0**112, 1.0, 0.0, float("nan"), float("inf")]).repeat(8)[None, None].to(torch.bfloat16).cuda()
+    for e in range(121, 127):                                  # codes 248 to 253
+        cache = Cache(rng, 2, 1, 64, fmt, exps=(e, e + 1))
+        cache.append(x, x.flip(2), [64 + 5])
+        cache.check(e)
+        assert (cache.exps[0] == e).all()
+    for e in (127, 128):                                       # codes 254, 255
+        cache = Cache(rng, 2, 1, 64, fmt, exps=(e, e + 1))
+        pe.peagle_cache_append_scaled(pe.CacheShape(1, 1, 64, 2), x, x, torch.tensor([64 + 5], device="cuda"), *cache.pages, *cache.scales)
+        for values in cache.values:
+            values[1, 0, 5] = np.where(np.isfinite(bf16_to_f64(x)[0, 0]), 0.0, np.nan)
+        cache.check(e)
+
+
 def test_append_adds_one_token_at_a_time():
     """A page filled by 64 calls with values that grow and shrink: the scale only grows, what is held is rounded again."""
     print("case append token by token", flush=True)

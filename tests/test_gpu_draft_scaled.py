@@ -487,3 +487,75 @@ def test_draft_scaled_large_new_values_under_keys_that_stand_out(D):
     for c in range(2):
         ro, rl = r.oracle(c)
         assert np.isfinite(o[c]).all() and rel_l2(o[c], ro) <= REL and max_abs(lse[c], rl) <= LSE_ABS, c
+
+
+class OneTokenEach:
+    """Requests of one cached token each, in a page of its own, which has all the weight: O is its value.  It scores 300 above the
+    new key."""
+
+    def __init__(self, C, Hkv, D, fmt):
+        q = torch.zeros((C, 1, Hkv, D), dtype=torch.bfloat16, device="cuda")
+        k, self.v_new = torch.zeros_like(q), torch.zeros_like(q)
+        q[..., 0], k[..., 0] = 300.0, -1.0
+        self.q, self.k, self.fmt, self.shape = q, k, fmt, pe.DecodeShape(C, 1, Hkv, Hkv, D, C, 1, 1.0)
+        keys = torch.zeros((C, Hkv, 64, D), device="cuda")
+        keys[..., 0] = 1.0
+        self.pages = [keys.to(TYPES[fmt]), torch.full(keys.shape, 0x7F, dtype=torch.uint8, device="cuda").view(TYPES[fmt])]
+        self.scales = [torch.full((C, Hkv), 127, dtype=torch.uint8, device="cuda").view(E8M0) for _ in range(2)]
+
+    def run(self):
+        s = self.shape
+        table, lens = torch.arange(s.C, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.ones(s.C, dtype=torch.int32, device="cuda")
+        o, lse, status = torch.empty_like(self.q), torch.empty((s.C, s.Hq, 1), device="cuda"), torch.empty_like(lens)
+        ws = torch.empty(pe.peagle_draft_decode_scaled_workspace_bytes(s), dtype=torch.uint8, device="cuda")
+        pe.peagle_draft_decode_scaled(s, self.q, self.k, self.v_new, *self.pages, *self.scales, table, lens, o, lse, status, ws)
+        torch.cuda.synchronize()
+        assert not status.any()
+        return bf16_to_f64(o)[:, 0]
+
+
+def _as_widened(x):
+    """Products of codes and scales as the step uses them: zero below bf16's normal numbers, infinite beyond them."""
+    return np.where(np.abs(x) >= 2.0**128, np.copysign(np.inf, x), np.where(np.abs(x) < 2.0**-126, 0.0, x))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_draft_scaled_widens_every_code_with_every_scale(D, fmt):
+    """All 256 codes of values under all 256 codes of scales: exact wherever the product is a normal bf16 number."""
+    print(f"case scaled every code and scale D={D} {fmt}", flush=True)
+    r = OneTokenEach(256, 256 // D, D, fmt)
+    every = torch.arange(256, dtype=torch.int32).to(torch.uint8)
+    r.pages[1].view(torch.uint8)[:, :, 0, :] = every.view(256 // D, D).cuda()
+    r.scales[1].view(torch.uint8).copy_(every[:, None].cuda())
+    o = r.run().reshape(256, 256)
+    codes = every.view(TYPES[fmt]).double().numpy()
+    exact = np.ldexp(codes[None], np.arange(256)[:, None] - 127)
+    exact[255] = np.nan
+    assert np.array_equal(o, _as_widened(exact), equal_nan=True)
+    finite, (low, high) = codes[np.isfinite(codes)], {"e4m3": (10, 246), "e5m2": (17, 239)}[fmt]
+    inside = np.ldexp(finite[None], np.arange(low, high + 1)[:, None] - 127)
+    assert np.array_equal(_as_widened(inside), inside)
+    for beyond in (low - 1, high + 1):  # (the range that the header names is the largest)
+        outside = np.ldexp(finite, beyond - 127)
+        assert not np.array_equal(_as_widened(outside), outside)
+
+
+@pytest.mark.parametrize("fmt,first", [("e4m3", 1.9375), ("e5m2", 1.875)])
+def test_append_and_draft_of_the_largest_values(fmt, first):
+    """The largest bf16 values are rounded to 2^128 from `first` * 2^127 on, which the drafting step shows as an infinity; what is
+    smaller stays finite."""
+    print(f"case scaled largest values {fmt}", flush=True)
+    x = np.array([1.75, 1.7578125, first - 2.0**-7, first, 1.9921875, -1.9921875, -1.75]) * 2.0**127
+    r = OneTokenEach(len(x), 2, 64, fmt)
+    rows = torch.from_numpy(x).float().to(torch.bfloat16).cuda()[:, None, None].expand(len(x), 2, 64).contiguous()
+    slots = torch.arange(len(x), device="cuda") * 64
+    pools, scales = [r.pages[0].clone(), r.pages[1]], [r.scales[0].clone(), r.scales[1]]  # (the keys stay what they are)
+    pe.peagle_cache_append_scaled(pe.CacheShape(len(x), 2, 64, len(x)), rows, rows, slots, *pools, *scales)
+    o = r.run()
+    exps = np.array([orc.scale_exponent(abs(v), fmt) for v in x])
+    assert np.array_equal(r.scales[1].view(torch.uint8).cpu().numpy().astype(int) - 127, np.stack([exps, exps], 1))
+    assert exps.max() == {"e4m3": 120, "e5m2": 113}[fmt]
+    want = _as_widened(np.array([orc.f8_round(v * 2.0**-e, fmt) * 2.0**e for v, e in zip(x, exps)]))
+    assert np.array_equal(o, np.broadcast_to(want[:, None, None], o.shape))
+    assert np.array_equal(np.isinf(want), np.abs(x) >= first * 2.0**127)
