@@ -130,6 +130,28 @@ def test_plan_with_requests_that_cannot_be_served(C, rows):
     assert (want["status"] == 2).any() or left > 0
 
 
+@pytest.mark.parametrize("C,first_short,ended,pad", [(50, 20, 0.0, 40), (50, 0, 0.0, 6000), (50, 40, 0.05, 40), (1024, 900, 0.1, 0),
+                                                     (1500, 600, 0.0, 10), (1500, 1200, 0.0, 10), (2500, 1800, 0.1, 3000), (2500, 2200, 0.0, 10)])
+def test_plan_when_the_pages_run_out(C, first_short, ended, pad):
+    """The list ends inside the pages that one request lacks, in a launch that writes the slots itself, in two, and in each of
+    several rounds of 1,024 requests: that request and all later ones that lack any get none, those that lack none are served."""
+    print(f"case plan short C={C} at {first_short}", flush=True)
+    rng = np.random.default_rng(C + first_short)
+    ctx, new, held, free, count, table = _state(rng, C, 300, 130, 0, ended=ended, rolled_back=0.0)
+    still = (rng.random(C) < 0.3) & (ctx > 0) & (ctx % 64 != 0)
+    new[still] = 1                                        # lacks no page
+    lacks, given = np.maximum(_pages(ctx + new) - held, 0), int(np.maximum(held - _pages(ctx + new), 0).sum())
+    f = next(c for c in range(first_short, C) if lacks[c] > 0)
+    there = int(lacks[:f].sum()) + int(lacks[f]) - 1 - given
+    assert 0 <= there < count
+    p = Plan(ctx, new, held, free, there, table, int(new.sum()) + pad)
+    p.call()
+    want = p.check((C, f))
+    assert (want["status"][:f] == 0).all() and want["status"][f] == 2
+    assert ((want["status"] == 2) == ((lacks > 0) & (np.arange(C) >= f))).all() and (want["status"][f + 1:] == 0).any()
+    assert want["free_count"][0] == lacks[f] - 1
+
+
 def test_plan_over_the_life_of_a_batch():
     """Admission, steps with accepted and rejected drafts, ends: the pool's pages are at every moment either held or free, each
     once, and when all requests have ended the list holds all of them."""
