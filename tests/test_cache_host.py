@@ -167,3 +167,28 @@ def test_scaled_draft_refuses_formats_pointers_and_workspaces():
     for n in ("q_new", "k_new", "v_new", "k_pages", "v_pages", "o", "workspace"):
         assert _draft_call(**{n: C.c_void_p(264)}) == EINVAL, n
     assert _draft_call(workspace=None) == EWORKSPACE and _draft_call(ws_bytes=16) == EWORKSPACE
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [1, 32, 33, 64, 96, 97, 128])
+def test_scaled_draft_workspaces_up_to_the_largest_shapes(rows, D):
+    """What a workspace holds, at the ends of every dimension: two records of rows x (D + 4) floats for each workgroup that shares a
+    KV head's work, and eight bytes a request.  There are no more workgroups than two for each of 256 compute units, or one a head."""
+    pad256 = lambda n: -(-n // 256) * 256
+    rows_pad = -(-rows // 32) * 32
+    for C_ in (1, 2, 64, 1024, 1025, 65535):
+        for Hkv in (1, 3, 8, 513, 65535):
+            for max_pages in (1, 16, 17, 64, 65, 1023, 1 << 20, 1 << 24):
+                shape = pe.DecodeShape(C_, 1, rows * Hkv, Hkv, D, 1 << 30, max_pages)
+                total = pe.peagle_draft_decode_scaled_workspace_bytes(shape)
+                size = lambda shares: pad256(2 * Hkv * shares * rows_pad * D * 4) + pad256(2 * Hkv * shares * rows_pad * 16) + pad256(8 * C_)
+                most = -(-512 // Hkv)
+                assert any(total == size(s) for s in range(most + 1)), (C_, Hkv, max_pages, total)
+                if C_ > 1024 or max_pages == 1 or C_ * max_pages > 1 << 30:
+                    assert total == size(0), (C_, Hkv, max_pages)
+
+
+def test_plan_workspaces_up_to_the_largest_shapes():
+    for C_ in (1, 16, 17, 1024, 65535):
+        for other in (1, 1 << 24):
+            assert pe.peagle_cache_plan_workspace_bytes(pe.PlanShape(C_, other, 1 << 30, 1 << 30)) == -(-16 * C_ // 256) * 256
