@@ -559,3 +559,31 @@ def test_append_and_draft_of_the_largest_values(fmt, first):
     want = _as_widened(np.array([orc.f8_round(v * 2.0**-e, fmt) * 2.0**e for v, e in zip(x, exps)]))
     assert np.array_equal(o, np.broadcast_to(want[:, None, None], o.shape))
     assert np.array_equal(np.isinf(want), np.abs(x) >= first * 2.0**127)
+
+
+@pytest.mark.parametrize("C,ctx,columns,K,Hq,Hkv,D", [(16, 1000, 320, 7, 64, 8, 64), (3, 70, 1024, 5, 32, 4, 128), (1, 0, 300, 1, 4, 2, 64), (70, 300, 90, 8, 16, 1, 128)])
+def test_draft_scaled_on_tables_wider_than_any_context(C, ctx, columns, K, Hq, Hkv, D):
+    """Tables as wide as the longest context that a server permits: the division of the work sees the width, the results do not."""
+    print(f"case scaled wide table C={C} columns={columns} D={D}", flush=True)
+    rng = np.random.default_rng(columns)
+    r = ScaledRun(tuple(int(x) for x in rng.integers(0, ctx + 1, C)), K, Hq, Hkv, D, "e4m3", 4400 + C)
+    r.table = np.pad(r.table, ((0, 0), (0, columns - r.shape.max_pages)), constant_values=-1)
+    r.bt = torch.from_numpy(r.table).cuda()
+    r.shape = pe.DecodeShape(C, K, Hq, Hkv, D, r.shape.n_pages, columns)
+    r.ws = torch.empty(pe.peagle_draft_decode_scaled_workspace_bytes(r.shape), dtype=torch.uint8, device="cuda").fill_(0x7F)
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    r.check(o, lse, "wide", range(0, C, max(1, C // 8)))
+
+
+@pytest.mark.parametrize("C", [999, 1024, 1025])
+def test_draft_scaled_of_a_thousand_requests(C):
+    """The most requests whose pages are shared among workgroups, and one more, which take a workgroup each."""
+    print(f"case scaled C={C}", flush=True)
+    rng = np.random.default_rng(C)
+    lens = rng.integers(0, 200, C)
+    lens[0], lens[500], lens[C - 1] = 5000, 4700, 4321
+    r = ScaledRun(tuple(int(x) for x in lens), 2, 2, 1, 64, "e5m2", C, shared=30)
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    r.check(o, lse, "thousand", (0, 1, 15, 16, 17, 499, 500, 501, C // 2, C - 2, C - 1))
