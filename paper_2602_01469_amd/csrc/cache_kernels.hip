@@ -281,8 +281,8 @@ __device__ __forceinline__ int scale_code(uint32_t amax) {
 // per_wave consecutive tokens (most tokens begin none; the slots of the 64 behind its first are all it needs) and stores each: all
 // its rows are loaded before the first is waited for, their largest value gives the scale, and what the page holds before the run
 // is turned to the new scale if that is larger.  Every value is read and written once, so bandwidth bounds a large call (16 prompts
-// of 203 to 16001 tokens, 4 heads of 128: 404 MB in 83 us on MI355X, 4.9 TB/s, the rate of a large copy), a launch and memory round
-// trips (slots; rows and the old scale) a small one (256 requests' 1 to 8 tokens: 5.1 us).  The waves of a workgroup take chunks
+// of 203 to 16001 tokens, 4 heads of 128: 399 MB in 84 us on MI355X, 4.8 TB/s, the rate of a large copy), a launch and memory round
+// trips (slots; rows and the old scale) a small one (256 requests' 1 to 8 tokens: 5.1 us; 11.8 where every page's scale grows).  The waves of a workgroup take chunks
 // that follow each other, so that the workgroups of a prompt, whose runs begin 64 tokens apart, are equally busy: with the heads
 // there instead, a prompt of 3891 tokens took 9.8 us rather than 5.8, as most XCDs had none.
 constexpr int kAppendWaves = 4;

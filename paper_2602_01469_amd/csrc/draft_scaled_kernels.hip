@@ -733,6 +733,11 @@ constexpr int kCus = 256;  // compute units of the device
 //          workgroup to work meanwhile.)  By request likewise where a CU gets one workgroup anyway: 40 of 300 to 2000 with 24 rows 16.7
 //          against 18.7, with 128 rows 27.5 against 26.9; with several for each CU two side by side are better: 100 of 100 to 1000
 //          with 128 rows 27.9 against 33.9.
+//   C > 1024   by request, as every workgroup would look through all lengths: 120 against 132 for 2000 of 500 to 3000 with one KV head, no
+//          difference with several.  A long request among short ones pays for it: 135 against 57 for one of 20000 among 1500 of 100 to 1000.
+// The rule sees the table's width; lengths are on the device.  In a table wider than they need, shares and their merge are taken where
+// a workgroup for each request would be faster: with 320 columns 17.7 instead of 12.5 for 16 of 1000, 26.3 instead of 18.8 for 32 of
+// 1000 to 2000, 17.7 instead of 13.6 for 4 of 2048 to 4096 (two workgroups a CU instead of one); nothing for 64 of 512 to 8192.
 ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
   ShareRule r;
   r.waves = D == 64 && blocks == 1 ? 8 : 4;
