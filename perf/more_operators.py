@@ -263,7 +263,7 @@ def prepare(case, seed):
         n_pages = s["k_pages"].shape[0]
         if case["kind"] == "draft":
             s["shape"] = pe.DecodeShape(case["C"], case["K"], case["Hq"], case["Hkv"], case["D"], n_pages, s["table"].shape[1])
-            s["ws"] = torch.empty(pe.peagle_draft_decode_fp4_workspace_bytes(s["shape"]), dtype=torch.uint8, device="cuda")
+            s["ws"] = torch.empty(pe.peagle_draft_decode_block_scaled_workspace_bytes(s["shape"]), dtype=torch.uint8, device="cuda")
         else:
             s["shape"] = pe.CacheShape(s["slots"].numel(), case["Hkv"], case["D"], n_pages)
     return s
@@ -322,10 +322,10 @@ def _run_own(s):
     kind = s["case"]["kind"]
     cache = s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"]
     if kind == "draft":
-        pe.peagle_draft_decode_fp4(s["shape"], s["q"], s["k"], s["v"], *cache, s["table"], s["ctx"], s["o"], s["lse"], s["status"], s["ws"])
+        pe.peagle_draft_decode_block_scaled(s["shape"], s["q"], s["k"], s["v"], *cache, s["table"], s["ctx"], s["o"], s["lse"], s["status"], s["ws"])
         return {n: s[n] for n in ("o", "lse", "status")}
     if kind == "append":
-        pe.peagle_cache_append_fp4(s["shape"], s["k"], s["v"], s["slots"], *cache)
+        pe.peagle_cache_append_block_scaled(s["shape"], s["k"], s["v"], s["slots"], *cache)
     pe.peagle_cache_read(s["shape"], s["slots"], *cache, s["k_out"], s["v_out"])
     return {n: s[n] for n in (("k_out", "v_out", "k_scale", "v_scale") if kind == "append" else ("k_out", "v_out"))}
 
