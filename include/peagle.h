@@ -488,6 +488,52 @@ int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t forma
                                const void* v_scale, const int32_t* block_table, const int32_t* ctx_len, void* o, float* lse,
                                int32_t* status, void* workspace, size_t ws_bytes, void* stream);
 
+/*
+ * The same cache in 4 bits: 17/32 byte a value.  A value is its code of the type E2M1 times a scale that 32 consecutive features of
+ * a token's KV head share (K and V apart), a power of two kept as its code (E8M0).  The plan, pages and block tables are those above.
+ *
+ *   pools    8-bit [n_pages, Hkv, 64, D/2]: the lower four bits of byte i hold feature 2i, the upper four feature 2i + 1; sign,
+ *            then 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes 0 to 7
+ *   scales   uint8 [n_pages, Hkv, 64, D/32]: 2^(code - 127); any code, 255 is NaN (the block's 32 values are)
+ *
+ * peagle_cache_append_block_scaled stores new tokens: the arguments of peagle_cache_append_scaled (shape->format has to be
+ * PEAGLE_CACHE_E2M1; the scales 16-byte aligned too), of which these differ:
+ *
+ *   A block's scale is the smallest power of two, at least 2^-100, that brings its largest value to 6 or below; values are rounded
+ *   to nearest, ties to the even code.  A block that holds an infinity or NaN gets the scale code 255 and codes of zero.  Tokens do
+ *   not depend on each other, and nothing that the cache holds of others changes.  Of two tokens of a call with the same slot it is
+ *   not defined which one's codes and which one's scales remain.  No call makes a scale code below 27 or, 255 apart, above 253.
+ */
+#define PEAGLE_CACHE_E2M1 2 /* 4 bits: sign, 2 of exponent, 1 of fraction; no infinity, no NaN */
+int peagle_cache_append_block_scaled(const peagle_cache_shape_t* shape, const void* k_new, const void* v_new, const int64_t* slots,
+                                     void* k_pages, void* v_pages, void* k_scale, void* v_scale, void* stream);
+
+/*
+ * Tokens of a cache of any of the three types as bf16 rows: a prefix for the next chunk of its prompt, a request that moves to
+ * another machine or to the bf16 cache.
+ *
+ *   shape            as for an append of n_tokens; k_stride, v_stride are those of the results
+ *   slots            device, int64 [n_tokens]: 64 * page + place in the page, in any order and number
+ *   k_pages ... v_scale   device: a cache of the type shape->format as above (4 bits: scales 16-byte aligned)
+ *   k_out, v_out     device, bf16 [n_tokens] rows of Hkv x D, 16-byte aligned (out; what stands between rows is left).  A token
+ *                    whose slot is outside [0, 64 * n_pages) becomes zeros
+ *
+ * Codes times scales as the drafting steps widen them, exact wherever the product is a bf16 number.
+ */
+int peagle_cache_read(const peagle_cache_shape_t* shape, const int64_t* slots, const void* k_pages, const void* v_pages,
+                      const void* k_scale, const void* v_scale, void* k_out, void* v_out, void* stream);
+
+/*
+ * peagle_draft_decode_scaled on the 4-bit cache: the same shape, arguments and results; the scales are 16-byte aligned.  Codes
+ * become bf16 without rounding; products are normal numbers for scale codes 2 to 252.  Smaller ones are zero, those from 2^128 on
+ * infinite, which an append makes of values from 1.75 * 2^127 on only.
+ */
+size_t peagle_draft_decode_block_scaled_workspace_bytes(const peagle_decode_shape_t* shape);
+int peagle_draft_decode_block_scaled(const peagle_decode_shape_t* shape, const void* q_new, const void* k_new, const void* v_new,
+                                     const void* k_pages, const void* v_pages, const void* k_scale, const void* v_scale,
+                                     const int32_t* block_table, const int32_t* ctx_len, void* o, float* lse, int32_t* status,
+                                     void* workspace, size_t ws_bytes, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* peagle_strerror(int status);
 

@@ -551,6 +551,52 @@ def cache_append(x: np.ndarray, slots: np.ndarray, pages: np.ndarray, exps: np.n
         t = end
 
 
+F4_VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])  # of the codes 0 to 7 of E2M1; 8 to 15 are their negatives
+F4_BLOCK = 32                                                     # features that share a scale
+
+
+def f4_codes(x: np.ndarray) -> np.ndarray:
+    """Codes of x rounded to the nearest value of E2M1, halfway to the even code; |x| at most 6 (zero keeps its sign)."""
+    x = np.asarray(x, dtype=np.float64)
+    size = np.abs(x)
+    assert (size <= 6).all()
+    away = np.abs(size[..., None] - F4_VALUES)
+    near = away == away.min(-1, keepdims=True)
+    low, high = near.argmax(-1), 7 - near[..., ::-1].argmax(-1)
+    return np.where(low % 2 == 0, low, high) + 8 * np.signbit(x)
+
+
+def f4_widen(codes: np.ndarray) -> np.ndarray:
+    codes = np.asarray(codes)
+    return np.where(codes > 7, -1.0, 1.0) * F4_VALUES[codes % 8]
+
+
+def cache_append_blocks(x: np.ndarray, slots: np.ndarray, codes: np.ndarray, scales: np.ndarray) -> None:
+    """Stores x [n, H, D] at `slots` of a 4-bit cache (page * 64 + place; outside the pool: not stored), in place.  codes
+    [n_pages, H, 64, D] of E2M1, scales [n_pages, H, 64, D / 32]: 127 + e of the smallest 2^e >= 2^-100 that brings the largest
+    of 32 features to 6 or below; a block that holds an infinity or NaN: 255, and codes of zero."""
+    for t, slot in enumerate(np.asarray(slots, dtype=np.int64)):
+        if not 0 <= slot < len(codes) * PAGE_TOKENS:
+            continue
+        page, at = divmod(int(slot), PAGE_TOKENS)
+        for h in range(x.shape[1]):
+            for b, block in enumerate(np.asarray(x[t, h], dtype=np.float64).reshape(-1, F4_BLOCK)):
+                where = slice(b * F4_BLOCK, (b + 1) * F4_BLOCK)
+                if not np.isfinite(block).all():
+                    scales[page, h, at, b], codes[page, h, at, where] = 255, 0
+                    continue
+                e = MIN_SCALE_EXPONENT
+                while np.abs(block).max() > 6 * 2.0 ** e:
+                    e += 1
+                scales[page, h, at, b], codes[page, h, at, where] = 127 + e, f4_codes(block * 2.0 ** -e)
+
+
+def cache_values_blocks(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """What a 4-bit cache stands for; a scale of 255 is NaN."""
+    scales = np.repeat(np.asarray(scales, dtype=np.int64), F4_BLOCK, -1)
+    return np.where(scales == 255, np.nan, f4_widen(codes) * np.exp2(scales - 127.0))
+
+
 def cache_plan(ctx_len, new_len, held, free_pages, free_count: int, table, max_tokens: int) -> Dict[str, np.ndarray]:
     """Request by request: pages that a request no longer needs go on the list (last request and block first), then each takes
     what it lacks off its end; slots of the new tokens.  Returns all results; the arguments are left as they are."""

@@ -57,6 +57,8 @@ EXPORTS = [
     "peagle_draft_decode_static",
     "peagle_cache_plan_workspace_bytes", "peagle_cache_plan", "peagle_cache_append_scaled",
     "peagle_draft_decode_scaled_workspace_bytes", "peagle_draft_decode_scaled",
+    "peagle_cache_append_block_scaled", "peagle_cache_read",
+    "peagle_draft_decode_block_scaled_workspace_bytes", "peagle_draft_decode_block_scaled",
     "peagle_attn_step_profiled", "peagle_measure_mfma_ceiling", "peagle_measure_mfma_ceiling_random", "peagle_device_info", "peagle_strerror",
 ]
 
@@ -155,6 +157,15 @@ def load_library():
     lib.peagle_draft_decode_scaled.argtypes = [C.POINTER(_DecodeShapeC), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
                                                vp]
     lib.peagle_draft_decode_scaled.restype = C.c_int
+    lib.peagle_cache_append_block_scaled.argtypes = [C.POINTER(_CacheShapeC), vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.peagle_cache_append_block_scaled.restype = C.c_int
+    lib.peagle_cache_read.argtypes = [C.POINTER(_CacheShapeC), vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.peagle_cache_read.restype = C.c_int
+    lib.peagle_draft_decode_block_scaled_workspace_bytes.argtypes = [C.POINTER(_DecodeShapeC)]
+    lib.peagle_draft_decode_block_scaled_workspace_bytes.restype = sz
+    lib.peagle_draft_decode_block_scaled.argtypes = [C.POINTER(_DecodeShapeC), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
+                                                     vp]
+    lib.peagle_draft_decode_block_scaled.restype = C.c_int
     lib.peagle_measure_mfma_ceiling.argtypes = [vp, C.POINTER(C.c_float)]
     lib.peagle_measure_mfma_ceiling.restype = C.c_int
     lib.peagle_measure_mfma_ceiling_random.argtypes = [vp, C.POINTER(C.c_float)]
@@ -647,13 +658,14 @@ def peagle_cache_plan(shape: PlanShape, ctx_len, new_len, pages_held, free_pages
 
 
 class CacheShape:
-    """Shape of an append to a paged cache held in 8 bits: n_tokens new tokens; the pools' type says which one it is."""
+    """Shape of an append to a paged cache held in 8 or 4 bits, or of reading one: n_tokens tokens; the pools' type says which
+    one it is."""
 
     def __init__(self, n_tokens: int, Hkv: int, D: int, n_pages: int):
         self.n_tokens, self.Hkv, self.D, self.n_pages = n_tokens, Hkv, D, n_pages
 
 
-CACHE_E4M3, CACHE_E5M2 = 0, 1
+CACHE_E4M3, CACHE_E5M2, CACHE_E2M1 = 0, 1, 2
 
 
 def _cache_pools(device, k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: int, D: int):
@@ -730,6 +742,79 @@ def peagle_draft_decode_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages,
         workspace.data_ptr(), workspace.numel(), _stream_on(dev, stream))
     if rc != 0:
         raise PeagleError(rc, "peagle_draft_decode_scaled")
+
+
+def _block_pools(device, k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: int, D: int):
+    """The pointers of a 4-bit cache's pools and scales."""
+    import torch
+    f4, e8 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu
+    pool, scales = (n_pages, Hkv, 64, D // 2), (n_pages, Hkv, 64, D // 32)
+    return (_ptr_on(device, k_pages, "k_pages", f4, pool), _ptr_on(device, v_pages, "v_pages", f4, pool),
+            _ptr_on(device, k_scale, "k_scale", e8, scales), _ptr_on(device, v_scale, "v_scale", e8, scales))
+
+
+def peagle_cache_append_block_scaled(shape: CacheShape, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream=None) -> None:
+    """Stores k_new, v_new [n_tokens, Hkv, D] (a token's heads contiguous, tokens any multiple of 8 elements apart) at `slots` of a
+    4-bit cache: pools of torch.float4_e2m1fn_x2 [n_pages, Hkv, 64, D / 2], scales of torch.float8_e8m0fnu [n_pages, Hkv, 64,
+    D / 32]."""
+    import torch
+    s, dev = shape, k_pages.get_device()
+    pools = _block_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    rows = (s.n_tokens, s.Hkv, s.D)
+    k, k_stride = _rows_ptr(dev, k_new, "k_new", torch.bfloat16, rows)
+    v, v_stride = _rows_ptr(dev, v_new, "v_new", torch.bfloat16, rows)
+    at = _ptr_on(dev, slots, "slots", torch.int64, (s.n_tokens,))
+    c = _CacheShapeC(s.n_tokens, s.Hkv, s.D, s.n_pages, CACHE_E2M1, k_stride, v_stride)
+    rc = load_library().peagle_cache_append_block_scaled(C.byref(c), k, v, at, *pools, _stream_on(dev, stream))
+    if rc != 0:
+        raise PeagleError(rc, "peagle_cache_append_block_scaled")
+
+
+def peagle_cache_read(shape: CacheShape, slots, k_pages, v_pages, k_scale, v_scale, k_out, v_out, stream=None) -> None:
+    """The tokens at `slots` of an 8-bit or 4-bit cache as bf16 rows k_out, v_out [n_tokens, Hkv, D] (which may stand apart as
+    those of an append may); zeros for slots outside the pools."""
+    import torch
+    s, dev = shape, k_pages.get_device()
+    if k_pages.dtype is torch.float4_e2m1fn_x2:
+        fmt, pools = CACHE_E2M1, _block_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    else:
+        fmt, *pools = _cache_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    rows = (s.n_tokens, s.Hkv, s.D)
+    k, k_stride = _rows_ptr(dev, k_out, "k_out", torch.bfloat16, rows)
+    v, v_stride = _rows_ptr(dev, v_out, "v_out", torch.bfloat16, rows)
+    at = _ptr_on(dev, slots, "slots", torch.int64, (s.n_tokens,))
+    c = _CacheShapeC(s.n_tokens, s.Hkv, s.D, s.n_pages, fmt, k_stride, v_stride)
+    rc = load_library().peagle_cache_read(C.byref(c), at, *pools, k, v, _stream_on(dev, stream))
+    if rc != 0:
+        raise PeagleError(rc, "peagle_cache_read")
+
+
+def peagle_draft_decode_block_scaled_workspace_bytes(shape: DecodeShape) -> int:
+    n = int(load_library().peagle_draft_decode_block_scaled_workspace_bytes(shape.c()))
+    if n == 0:
+        raise PeagleError(-3, "peagle_draft_decode_block_scaled_workspace_bytes")
+    return n
+
+
+def peagle_draft_decode_block_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages, v_pages, k_scale, v_scale, block_table, ctx_len,
+                                     o, lse, status, workspace, stream=None) -> None:
+    """peagle_draft_decode on a cache held in 4 bits, as peagle_cache_append_block_scaled stores it."""
+    import torch
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    s = shape
+    if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace: expected a contiguous uint8 GPU tensor")
+    dev = workspace.get_device()
+    pools = _block_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
+    rows, new = (s.C, s.K, s.Hq, s.D), (s.C, s.K, s.Hkv, s.D)
+    rc = load_library().peagle_draft_decode_block_scaled(
+        s.c(), _ptr_on(dev, q_new, "q_new", bf, rows), _ptr_on(dev, k_new, "k_new", bf, new), _ptr_on(dev, v_new, "v_new", bf, new),
+        *pools, _ptr_on(dev, block_table, "block_table", i32, (s.C, s.max_pages)), _ptr_on(dev, ctx_len, "ctx_len", i32, (s.C,)),
+        _ptr_on(dev, o, "o", bf, rows), _ptr_on(dev, lse, "lse", f32, (s.C, s.Hq, s.K)),
+        None if status is None else _ptr_on(dev, status, "status", i32, (s.C,)),
+        workspace.data_ptr(), workspace.numel(), _stream_on(dev, stream))
+    if rc != 0:
+        raise PeagleError(rc, "peagle_draft_decode_block_scaled")
 
 
 def peagle_measure_mfma_ceiling(stream=None, random_operands: bool = False) -> float:

@@ -792,17 +792,18 @@ extern "C" size_t peagle_draft_decode_scaled_workspace_bytes(const peagle_decode
   return check_decode(shape) == PEAGLE_OK ? decode_scaled_ws(shape).total : 0;
 }
 
-extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,
-                                          const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale,
-                                          const void* v_scale, const int32_t* block_table, const int32_t* ctx_len, void* o,
-                                          float* lse, int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
-  const int rc = check_decode(shape);
-  if (rc != PEAGLE_OK) return rc;
-  if (format != PEAGLE_CACHE_E4M3 && format != PEAGLE_CACHE_E5M2) return PEAGLE_EUNSUPPORTED;
+namespace {
+
+int draft_scaled_impl(const peagle_decode_shape_t* shape, peagle::CacheType cache, const void* q_new, const void* k_new,
+                      const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale, const void* v_scale,
+                      const int32_t* block_table, const int32_t* ctx_len, void* o, float* lse, int32_t* status, void* workspace,
+                      size_t ws_bytes, void* stream) {
   if (!q_new || !k_new || !v_new || !k_pages || !v_pages || !k_scale || !v_scale || !block_table || !ctx_len || !o || !lse)
     return PEAGLE_ENULL;
   if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o))
     return PEAGLE_EINVAL;
+  // (scales of 4-bit codes are copied four at a time)
+  if (cache == peagle::CacheType::kE2M1 && (!aligned16(k_scale) || !aligned16(v_scale))) return PEAGLE_EINVAL;
   const ScaledWs w = decode_scaled_ws(shape);
   if (!workspace || ws_bytes < w.total) return PEAGLE_EWORKSPACE;
   if (!aligned16(workspace)) return PEAGLE_EINVAL;
@@ -813,8 +814,99 @@ extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, in
   p.v_pages = (const uint8_t*)v_pages;
   p.k_scale = (const uint8_t*)k_scale;
   p.v_scale = (const uint8_t*)v_scale;
-  return peagle::launch_draft_scaled(p, shape->D, format == PEAGLE_CACHE_E5M2, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK
-                                                                                                                 : PEAGLE_EHIP;
+  return peagle::launch_draft_scaled(p, shape->D, cache, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK : PEAGLE_EHIP;
+}
+
+}  // namespace
+
+extern "C" int peagle_draft_decode_scaled(const peagle_decode_shape_t* shape, int32_t format, const void* q_new, const void* k_new,
+                                          const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale,
+                                          const void* v_scale, const int32_t* block_table, const int32_t* ctx_len, void* o,
+                                          float* lse, int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_decode(shape);
+  if (rc != PEAGLE_OK) return rc;
+  if (format != PEAGLE_CACHE_E4M3 && format != PEAGLE_CACHE_E5M2) return PEAGLE_EUNSUPPORTED;
+  return draft_scaled_impl(shape, (peagle::CacheType)format, q_new, k_new, v_new, k_pages, v_pages, k_scale, v_scale, block_table,
+                           ctx_len, o, lse, status, workspace, ws_bytes, stream);
+}
+
+// The cache in 4 bits: stored, read back (the 8-bit types too), and drafted from.
+namespace {
+
+int check_rows(const peagle_cache_shape_t& s) {
+  if (s.n_tokens < 0 || s.Hkv < 1 || s.n_pages < 1) return PEAGLE_EINVAL;
+  if (s.D != 64 && s.D != 128) return PEAGLE_EUNSUPPORTED;
+  if (s.n_tokens > (1 << 28) || s.Hkv > 65535 || s.n_pages > (1 << 30)) return PEAGLE_EUNSUPPORTED;  // grid dimensions
+  const int64_t row = (int64_t)s.Hkv * s.D;
+  if (s.k_stride < row || s.v_stride < row || s.k_stride % 8 != 0 || s.v_stride % 8 != 0) return PEAGLE_EINVAL;
+  return PEAGLE_OK;
+}
+
+peagle::RowsParams rows_params(const peagle_cache_shape_t& s, const int64_t* slots, const void* k_rows, const void* v_rows,
+                               const void* k_pages, const void* v_pages, const void* k_scale, const void* v_scale) {
+  peagle::RowsParams p{};
+  p.slots = slots;
+  p.k_rows = (__bf16*)k_rows;
+  p.v_rows = (__bf16*)v_rows;
+  p.k_pages = (uint8_t*)k_pages;
+  p.v_pages = (uint8_t*)v_pages;
+  p.k_scale = (uint8_t*)k_scale;
+  p.v_scale = (uint8_t*)v_scale;
+  p.k_stride = s.k_stride;
+  p.v_stride = s.v_stride;
+  p.n_tokens = s.n_tokens;
+  p.Hkv = s.Hkv;
+  p.n_pages = s.n_pages;
+  return p;
+}
+
+}  // namespace
+
+extern "C" int peagle_cache_append_block_scaled(const peagle_cache_shape_t* shape, const void* k_new, const void* v_new,
+                                                const int64_t* slots, void* k_pages, void* v_pages, void* k_scale, void* v_scale,
+                                                void* stream) {
+  if (!shape) return PEAGLE_ENULL;
+  const int rc = check_rows(*shape);
+  if (rc != PEAGLE_OK) return rc;
+  if (shape->format != PEAGLE_CACHE_E2M1) return PEAGLE_EUNSUPPORTED;
+  if (!k_pages || !v_pages || !k_scale || !v_scale) return PEAGLE_ENULL;
+  if (shape->n_tokens == 0) return PEAGLE_OK;
+  if (!k_new || !v_new || !slots) return PEAGLE_ENULL;
+  for (const void* x : {k_new, v_new, (const void*)k_pages, (const void*)v_pages, (const void*)k_scale, (const void*)v_scale})
+    if (!aligned16(x)) return PEAGLE_EINVAL;
+  const peagle::RowsParams p = rows_params(*shape, slots, k_new, v_new, k_pages, v_pages, k_scale, v_scale);
+  return peagle::launch_cache_append_blocks(p, shape->D, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK : PEAGLE_EHIP;
+}
+
+extern "C" int peagle_cache_read(const peagle_cache_shape_t* shape, const int64_t* slots, const void* k_pages, const void* v_pages,
+                                 const void* k_scale, const void* v_scale, void* k_out, void* v_out, void* stream) {
+  if (!shape) return PEAGLE_ENULL;
+  const int rc = check_rows(*shape);
+  if (rc != PEAGLE_OK) return rc;
+  const int32_t f = shape->format;
+  if (f != PEAGLE_CACHE_E4M3 && f != PEAGLE_CACHE_E5M2 && f != PEAGLE_CACHE_E2M1) return PEAGLE_EUNSUPPORTED;
+  if (!k_pages || !v_pages || !k_scale || !v_scale) return PEAGLE_ENULL;
+  if (shape->n_tokens == 0) return PEAGLE_OK;
+  if (!slots || !k_out || !v_out) return PEAGLE_ENULL;
+  for (const void* x : {k_pages, v_pages, (const void*)k_out, (const void*)v_out})
+    if (!aligned16(x)) return PEAGLE_EINVAL;
+  if (f == PEAGLE_CACHE_E2M1 && (!aligned16(k_scale) || !aligned16(v_scale))) return PEAGLE_EINVAL;
+  const peagle::RowsParams p = rows_params(*shape, slots, k_out, v_out, k_pages, v_pages, k_scale, v_scale);
+  return peagle::launch_cache_read(p, shape->D, (peagle::CacheType)f, (hipStream_t)stream) == hipSuccess ? PEAGLE_OK : PEAGLE_EHIP;
+}
+
+extern "C" size_t peagle_draft_decode_block_scaled_workspace_bytes(const peagle_decode_shape_t* shape) {
+  return check_decode(shape) == PEAGLE_OK ? decode_scaled_ws(shape).total : 0;
+}
+
+extern "C" int peagle_draft_decode_block_scaled(const peagle_decode_shape_t* shape, const void* q_new, const void* k_new,
+                                                const void* v_new, const void* k_pages, const void* v_pages, const void* k_scale,
+                                                const void* v_scale, const int32_t* block_table, const int32_t* ctx_len, void* o,
+                                                float* lse, int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_decode(shape);
+  if (rc != PEAGLE_OK) return rc;
+  return draft_scaled_impl(shape, peagle::CacheType::kE2M1, q_new, k_new, v_new, k_pages, v_pages, k_scale, v_scale, block_table,
+                           ctx_len, o, lse, status, workspace, ws_bytes, stream);
 }
 
 extern "C" int peagle_measure_mfma_ceiling(void* stream, float* tflops) {

@@ -118,18 +118,21 @@ hipError_t launch_draft_decode(const DecodeParams& p, int D, hipStream_t stream)
 // number of pieces that the workspace has records for.
 int draft_pieces(int64_t wgs_per_piece, int max_pages, int laid_out, int D);
 
-// The drafting step on a cache that is held in 8 bits.
+// Types of what a scaled cache holds, as PEAGLE_CACHE_*.
+enum class CacheType { kE4M3 = 0, kE5M2 = 1, kE2M1 = 2 };
+
+// The drafting step on a cache that is held in 8 or 4 bits.
 struct ScaledDecodeParams {
   DecodeParams d;          // k_pages, v_pages, n_splits unused
-  const uint8_t* k_pages;  // [n_pages, Hkv, 64, D]
+  const uint8_t* k_pages;  // [n_pages, Hkv, 64, D]; 4 bits: [n_pages, Hkv, 64, D / 2]
   const uint8_t* v_pages;
-  const uint8_t* k_scale;  // [n_pages, Hkv] codes of powers of two
+  const uint8_t* k_scale;  // [n_pages, Hkv] codes of powers of two; 4 bits: [n_pages, Hkv, 64, D / 32]
   const uint8_t* v_scale;
   int2* pieces;            // workspace [C]: first of a request's records, number of them
   int shares, least_share, lead;  // filled by the launcher, as in ShareRule; [Hkv, shares, 2]
                            // records: d.part_o [rows_pad, D], d.part_ml [rows_pad, 4] reference, sums, flag
 };
-hipError_t launch_draft_scaled(const ScaledDecodeParams& p, int D, bool e5m2, hipStream_t stream);
+hipError_t launch_draft_scaled(const ScaledDecodeParams& p, int D, CacheType cache, hipStream_t stream);
 struct ShareRule {
   int shares;  // workgroups that share the work of a KV head (0: one for each request)
   int least;   // units that a workgroup takes at least

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "attn_kernels.h"
 #include "tilemap.h"
 
 namespace peagle {
@@ -48,5 +49,20 @@ struct AppendParams {
   int per_wave;           // filled by the launcher: tokens whose runs a wave looks for, a power of two up to 64
 };
 hipError_t launch_cache_append(const AppendParams& p, int D, bool e5m2, hipStream_t stream);
+
+// Tokens' rows and their places in a cache: stored in 4 bits, or read back from any type.
+struct RowsParams {
+  const int64_t* slots;  // [n_tokens]
+  __bf16* k_rows;        // [n_tokens] rows of Hkv x D, k_stride elements apart; not written by the append
+  __bf16* v_rows;
+  uint8_t* k_pages;      // [n_pages, Hkv, 64, D] or, with codes of 4 bits, [n_pages, Hkv, 64, D / 2]; not written by the read
+  uint8_t* v_pages;
+  uint8_t* k_scale;      // [n_pages, Hkv] or [n_pages, Hkv, 64, D / 32]
+  uint8_t* v_scale;
+  int64_t k_stride, v_stride;
+  int n_tokens, Hkv, n_pages;
+};
+hipError_t launch_cache_append_blocks(const RowsParams& p, int D, hipStream_t stream);
+hipError_t launch_cache_read(const RowsParams& p, int D, CacheType cache, hipStream_t stream);
 
 }  // namespace peagle

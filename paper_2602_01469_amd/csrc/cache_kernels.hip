@@ -386,7 +386,160 @@ __global__ __launch_bounds__(kAppendWaves * 64) void cache_append_kernel(AppendP
   }
 }
 
+// ------------------------------------------------------------------------------------- rows to 4 bits, and rows back
+
+// Eight features of a token a lane: D / 8 lanes a token's KV head, 64 / (D / 8) tokens a wave and step, kRowSteps steps a wave.  All
+// loads of a wave are issued before the first is used.
+constexpr int kRowSteps = 4, kRowWaves = 4;
+template <int D>
+struct RowLane {
+  static constexpr int kLanes = D / 8, kTokens = 64 / kLanes;
+  const bool is_v;
+  const int head, lane, chunk;  // chunk: which eight features
+  int64_t first;                // token of step 0
+  __device__ __forceinline__ explicit RowLane(const RowsParams& p)
+      : is_v((int)blockIdx.x >= p.Hkv), head(is_v ? (int)blockIdx.x - p.Hkv : (int)blockIdx.x), lane(threadIdx.x & 63), chunk(lane % kLanes) {
+    const int64_t wave = ((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * kRowWaves + (threadIdx.x >> 6);
+    first = wave * (kRowSteps * kTokens) + lane / kLanes;
+  }
+};
+
+// A block of 32 features of one token and KV head: the smallest scale 2^e that brings its largest value to 6 or below, the code of
+// each value times 2^-e.  Both come from integers and one instruction for two values: of the bits of |x| the largest tells the
+// exponent (6 is 1.5 times a power of two, so one more where the fraction is above 0.5).
+template <int D>
+__global__ __launch_bounds__(kRowWaves * 64) void cache_append_blocks_kernel(RowsParams p) {
+  using L = RowLane<D>;
+  const L at(p);
+  const __bf16* rows = (at.is_v ? p.v_rows : p.k_rows) + (size_t)at.head * D + at.chunk * 8;
+  const int64_t stride = at.is_v ? p.v_stride : p.k_stride, limit = (int64_t)p.n_pages * kKeysPerTile;
+  uint8_t* pages = at.is_v ? p.v_pages : p.k_pages;
+  uint8_t* scales = at.is_v ? p.v_scale : p.k_scale;
+  int64_t slot[kRowSteps];
+  u32x4 x[kRowSteps];
+#pragma unroll
+  for (int i = 0; i < kRowSteps; ++i) {
+    const int64_t t = at.first + i * L::kTokens;
+    slot[i] = -1;
+    x[i] = u32x4{0u, 0u, 0u, 0u};
+    if (t < p.n_tokens) {
+      slot[i] = p.slots[t];
+      x[i] = *reinterpret_cast<const u32x4*>(rows + t * stride);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowSteps; ++i) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = x[i][j];
+      amax = max(amax, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
+    }
+    amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xb1, 0xf, 0xf, true));  // the other lane of each pair,
+    amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0x4e, 0xf, 0xf, true));  // the other pair of each four
+    int code = (int)((amax + 0x3fu) >> 7) - 2;
+    code = code < 127 + kMinScaleExponent ? 127 + kMinScaleExponent : code;
+    const float scale = power_of(code);
+    uint32_t codes = 0;
+    auto two = [&](uint32_t w) { return __builtin_bit_cast(bf16x2, w); };
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, two(x[i][0]), scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, two(x[i][1]), scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, two(x[i][2]), scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, two(x[i][3]), scale, 3);
+    if (amax >= 0x7f80u) {  // an infinity or NaN: 4 bits have neither, the scale has NaN
+      code = 255;
+      codes = 0;
+    }
+    if (slot[i] < 0 || slot[i] >= limit) continue;
+    const size_t place = ((size_t)(slot[i] / kKeysPerTile) * p.Hkv + at.head) * kKeysPerTile + (size_t)(slot[i] % kKeysPerTile);
+    reinterpret_cast<uint32_t*>(pages)[place * (D / 8) + at.chunk] = codes;
+    if (at.chunk % 4 == 0) scales[place * (D / 32) + at.chunk / 4] = (uint8_t)code;
+  }
+}
+
+template <int D, CacheType T>
+__global__ __launch_bounds__(kRowWaves * 64) void cache_read_kernel(RowsParams p) {
+  using L = RowLane<D>;
+  constexpr bool kFour = T == CacheType::kE2M1;
+  const L at(p);
+  __bf16* rows = (at.is_v ? p.v_rows : p.k_rows) + (size_t)at.head * D + at.chunk * 8;
+  const int64_t stride = at.is_v ? p.v_stride : p.k_stride, limit = (int64_t)p.n_pages * kKeysPerTile;
+  const uint8_t* pages = at.is_v ? p.v_pages : p.k_pages;
+  const uint8_t* scales = at.is_v ? p.v_scale : p.k_scale;
+  u32x2 w[kRowSteps];
+  int code[kRowSteps];
+  int64_t slot[kRowSteps];
+#pragma unroll
+  for (int i = 0; i < kRowSteps; ++i) {
+    const int64_t t = at.first + i * L::kTokens;
+    slot[i] = t < p.n_tokens ? p.slots[t] : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < kRowSteps; ++i) {
+    w[i] = u32x2{0u, 0u};  // (zero, whatever the scale but NaN)
+    code[i] = 127;
+    if (slot[i] < 0 || slot[i] >= limit) continue;
+    const size_t page_head = (size_t)(slot[i] / kKeysPerTile) * p.Hkv + at.head;
+    const size_t place = page_head * kKeysPerTile + (size_t)(slot[i] % kKeysPerTile);
+    if (kFour) {
+      w[i][0] = reinterpret_cast<const uint32_t*>(pages)[place * (D / 8) + at.chunk];
+      code[i] = scales[place * (D / 32) + at.chunk / 4];
+    } else {
+      w[i] = reinterpret_cast<const u32x2*>(pages)[place * (D / 8) + at.chunk];
+      code[i] = scales[page_head];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowSteps; ++i) {
+    const int64_t t = at.first + i * L::kTokens;
+    if (t >= p.n_tokens) continue;
+    const float scale = __builtin_bit_cast(float, (uint32_t)code[i] << 23);
+    const uint32_t a = w[i][0], b = w[i][1];
+    u32x4 out;
+    auto put = [&](int j, bf16x2 v) { out[j] = __builtin_bit_cast(uint32_t, v); };
+    if (T == CacheType::kE2M1) {
+      put(0, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 0));
+      put(1, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 1));
+      put(2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 2));
+      put(3, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 3));
+    } else if (T == CacheType::kE5M2) {
+      put(0, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(a, scale, false));
+      put(1, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(a, scale, true));
+      put(2, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(b, scale, false));
+      put(3, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(b, scale, true));
+    } else {
+      put(0, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false));
+      put(1, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true));
+      put(2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false));
+      put(3, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true));
+    }
+    *reinterpret_cast<u32x4*>(rows + t * stride) = out;
+  }
+}
+
+dim3 rows_grid(const RowsParams& p, int D) {
+  const int64_t span = (int64_t)kRowWaves * kRowSteps * (64 / (D / 8)), spans = (p.n_tokens + span - 1) / span;
+  const unsigned y = (unsigned)(spans < 32768 ? spans : 32768);
+  return dim3((unsigned)(2 * p.Hkv), y, (unsigned)((spans + y - 1) / y));
+}
+
 }  // namespace
+
+hipError_t launch_cache_append_blocks(const RowsParams& p, int D, hipStream_t stream) {
+  auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows_grid(p, D), dim3(kRowWaves * 64), 0, stream, p); };
+  D == 64 ? run(cache_append_blocks_kernel<64>) : run(cache_append_blocks_kernel<128>);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const RowsParams& p, int D, CacheType cache, hipStream_t stream) {
+  auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows_grid(p, D), dim3(kRowWaves * 64), 0, stream, p); };
+  switch (cache) {
+    case CacheType::kE4M3: D == 64 ? run(cache_read_kernel<64, CacheType::kE4M3>) : run(cache_read_kernel<128, CacheType::kE4M3>); break;
+    case CacheType::kE5M2: D == 64 ? run(cache_read_kernel<64, CacheType::kE5M2>) : run(cache_read_kernel<128, CacheType::kE5M2>); break;
+    case CacheType::kE2M1: D == 64 ? run(cache_read_kernel<64, CacheType::kE2M1>) : run(cache_read_kernel<128, CacheType::kE2M1>); break;
+  }
+  return hipGetLastError();
+}
 
 hipError_t launch_cache_plan(const PlanParams& p, hipStream_t stream) {
   const bool one = p.C <= kPlanThreads && p.max_tokens <= 4096;

@@ -1,8 +1,9 @@
 // The inference-side drafting step (Sec. 2 of the paper) on a paged cache that is held in 8 bits with a power-of-two scale for
-// each page and KV head: the K new rows of each request see its cached keys and the new keys of their own chain.
+// each page and KV head, or in 4 bits with one for each token, KV head and 32 features: the K new rows of each request see its
+// cached keys and the new keys of their own chain.
 //
-// With k = 2^ek a and v = 2^ev b for the codes a, b of a page, S = scale Q K^T, P = 2^(S log2(e) - m), O = P V / sum P.  A code
-// has four significant bits or three, so that with its page's scale it is a bf16 number (zero where that would not be a normal one,
+// With k = 2^ek a and v = 2^ev b for the codes a, b, S = scale Q K^T, P = 2^(S log2(e) - m), O = P V / sum P.  A code
+// has four significant bits or fewer, so that with its scale it is a bf16 number (zero where that would not be a normal one,
 // infinite from 2^128 on): codes are widened to bf16, scale and all, by one instruction for two of them, between LDS and the
 // matrix instruction.  (The matrix instruction for 8-bit types, with queries split into two numbers of them, would need no widening
 // of keys, but its sums are not fp32 sums: 64 products of normal data came out 4e-5 of the largest sum off.)
@@ -18,19 +19,31 @@ namespace peagle {
 
 namespace {
 
+template <CacheType T>
+constexpr bool kFour = T == CacheType::kE2M1;  // two codes a byte
+
 // Eight codes, times `scale` (a power of two), as a matrix operand.
-template <bool E5M2>
+template <CacheType T>
 __device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float scale) {
   u32x4 u;
   auto two = [&](uint32_t w, auto high) {
     constexpr bool H = decltype(high)::value;
-    const bf16x2 x = E5M2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, H) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, H);
+    const bf16x2 x = T == CacheType::kE5M2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, H) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, H);
     return __builtin_bit_cast(uint32_t, x);
   };
   u[0] = two(a, std::false_type{});
   u[1] = two(a, std::true_type{});
   u[2] = two(b, std::false_type{});
   u[3] = two(b, std::true_type{});
+  return __builtin_bit_cast(bf16x8, u);
+}
+// Eight codes of 4 bits.  (Of the scale the instruction takes the exponent alone; 255 makes NaN of every code.)
+__device__ __forceinline__ bf16x8 widen4(uint32_t w, float scale) {
+  u32x4 u;
+  u[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  u[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  u[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  u[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
   return __builtin_bit_cast(bf16x8, u);
 }
 
@@ -45,11 +58,28 @@ __device__ __forceinline__ int swz8(int row) {
   const int r = row >> 1;
   return D == 64 ? (row >> 2) & 3 : (r & 4) | ((r & 1) << 1) | ((r >> 1) & 1);
 }
+// The same of rows of D / 2 bytes, codes of 4 bits, of which 16 lanes read the same chunk of 16 rows (eight, at D = 128 four, per
+// 256 bytes).
+template <int D>
+__device__ __forceinline__ int swz4(int row) {
+  return D == 64 ? (row >> 3) & 1 : (row >> 2) & 3;
+}
+template <int D, CacheType T>
+__device__ __forceinline__ int swz_codes(int row) {
+  return kFour<T> ? swz4<D>(row) : swz8<D>(row);
+}
+
+// Which eight features step i of the product with the keys takes in lanes of half g: those that follow each other in a 16-byte read
+// of the keys' codes, two steps' with codes of 8 bits, four steps' with codes of 4 bits (which so have one scale).
+template <CacheType T>
+__device__ __forceinline__ int q_chunk(int i, int g) {
+  return kFour<T> ? 8 * (i / 4) + 4 * g + i % 4 : 4 * (i / 2) + 2 * g + i % 2;
+}
 
 // State of RB blocks of 32 query rows: lane <-> row, registers <-> features 32 db + 8 (i / 4) + 4 g + i % 4.
 template <int D, int RB>
 struct Rows {
-  bf16x8 q[RB][D / 16];  // features 32 i + 16 g + 8 j .. + 8 of step 2 i + j
+  bf16x8 q[RB][D / 16];  // eight features of each step, see q_chunk()
   f32x16 o[RB][D / 32];
   float m[RB];           // reference of the exponents (log2)
   float l[RB], w[RB];    // sums over this lane's keys of the probabilities: as they are, and as they weigh the values
@@ -100,7 +130,7 @@ __device__ __forceinline__ uint32_t bytes_of(uint32_t keep) { return ((keep & 0x
 
 // 32 keys, staged with their values, of which the first n count.  The others are masked, and their codes of values made zero: a
 // probability of zero times an infinity, which E5M2 holds and any code becomes beyond bf16, would be NaN.
-template <int D, bool E5M2, int RB>
+template <int D, CacheType T, int RB>
 __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, const int (&k_off)[D / 32],
                                             const int (&v_off)[D / 32], float ks, float vs, float limit, int n, int g,
                                             float c) {
@@ -124,7 +154,7 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
   for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
-    const bf16x8 a0 = widen8<E5M2>(kw[i][0], kw[i][1], ks), a1 = widen8<E5M2>(kw[i][2], kw[i][3], ks);
+    const bf16x8 a0 = widen8<T>(kw[i][0], kw[i][1], ks), a1 = widen8<T>(kw[i][2], kw[i][3], ks);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       s[rb] = mfma32(a0, r.q[rb][2 * i], s[rb]);
@@ -153,11 +183,94 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) {
-      const bf16x8 a = widen8<E5M2>((uint32_t)vw[t][db][0], (uint32_t)vw[t][db][1], vs);
+      const bf16x8 a = widen8<T>((uint32_t)vw[t][db][0], (uint32_t)vw[t][db][1], vs);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(a, pb[rb][t], r.o[rb][db]);
     }
   __builtin_amdgcn_s_setprio(0);
+}
+
+// The same of codes of 4 bits.  Two neighbouring keys' values have scales of their own, so that the codes of one feature cannot be
+// widened as the product takes them, two keys at a time.  They are widened as they stand instead - lane <-> key, 32 features and
+// one scale, as the keys - and written to this wave's part of LDS as a tile of bf16 rows, which is read transposed as new keys' values
+// are.
+template <int D>
+struct Off4 {
+  int codes[D / 64], scale[D / 64];  // of a lane's 16-byte chunk j, features 32 (2 j + g) .. + 32 of key lane % 32, and its scale
+  int out[D / 64][4];                // of its eight features w in the tile
+  TrOff<D> tr;
+};
+template <int D, int RB>
+__device__ __forceinline__ void cached_keys4(Rows<D, RB>& r, const char* k_at, const char* v_at, const char* ks_at, const char* vs_at, char* tile,
+                                             const Off4<D>& off, int n, int ln, int g, float c) {
+  u32x4 kw[D / 64], vw[D / 64];
+  uint32_t ks[D / 64], vs[D / 64];
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    kw[j] = *reinterpret_cast<const u32x4*>(k_at + off.codes[j]);
+    ks[j] = *reinterpret_cast<const uint8_t*>(ks_at + off.scale[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    vw[j] = *reinterpret_cast<const u32x4*>(v_at + off.codes[j]);
+    vs[j] = *reinterpret_cast<const uint8_t*>(vs_at + off.scale[j]);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  if (n < 32) {  // (whatever stands behind the last key: zeros)
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      vs[j] = ln < n ? vs[j] : 127u;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) vw[j][w] = ln < n ? vw[j][w] : 0u;
+    }
+  }
+  bool large = false;
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) large |= vs[j] > (uint32_t)kFarScale && vs[j] != 255u;  // (NaN changes no bit of other features)
+  const float limit = __builtin_amdgcn_ballot_w64(large) != 0 ? kNearLimit : kFarLimit;
+  __builtin_amdgcn_s_setprio(1);
+  f32x16 s[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) s[rb] = zero16();
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t word = kw[j][w];
+      const bf16x8 a = widen4(word, __builtin_bit_cast(float, ks[j] << 23));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) s[rb] = mfma32(a, r.q[rb][4 * j + w], s[rb]);
+    }
+  __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t word = vw[j][w];
+      *reinterpret_cast<bf16x8*>(tile + off.out[j][w]) = widen4(word, __builtin_bit_cast(float, vs[j] << 23));
+    }
+  asm volatile("" : : : "memory");  // (the tile is this wave's, whose LDS accesses take place in their order)
+  if (n < 32) {
+    const uint32_t bits = ((1u << n) - 1) >> (4 * g);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
+  }
+  bf16x8 pb[RB][2];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) soft(r, rb, s[rb], c, limit, pb[rb]);
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const bf16x8 a = frag_tr<D>(tile, off.tr, 16 * t, db);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) r.o[rb][db] = mfma32(a, pb[rb][t], r.o[rb][db]);
+    }
+  __builtin_amdgcn_s_setprio(0);
+  asm volatile("" : : : "memory");
 }
 
 // Sixteen of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
@@ -165,14 +278,14 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
 // NaN: such values are taken out of the product and added to the rows that see them, from v_new (key 0 of the KV head, the next
 // one `stride` elements on).
 constexpr int kNewKeys = 16;
-template <int D, int RB>
+template <int D, CacheType T, int RB>
 __device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, int k0, int K, const __bf16* v_new, uint32_t stride,
                                          const int (&depth)[RB], float c) {
   const int lane = lane_id(), g = lane >> 5, row = lane % kNewKeys;
   bf16x8 ka[D / 16], va[D / 32];
   const TrOff<D> to = tr_offsets<D>(lane);
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(k_at + tile_off<D>(row, 4 * (i / 2) + 2 * g + i % 2));
+  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(k_at + tile_off<D>(row, q_chunk<T>(i, g)));
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) va[db] = frag_tr<D>(v_at, to, 0, db);
   __builtin_amdgcn_sched_barrier(0);
@@ -311,6 +424,23 @@ __device__ __forceinline__ T* held(T* x) {  // (as a pointer to global memory, w
   return (T*)g;
 }
 
+// A stream's share of LDS: a ring of slots of kTokens tokens each and, with codes of 4 bits, a tile for each of its waves.
+template <int D, CacheType T, int RB, int PARTS>
+struct Ring {
+  static constexpr bool kSmall = D == 64 && RB == 1;                // four waves a SIMD, otherwise two
+  static constexpr int kRow = kFour<T> ? D / 2 : D;                 // bytes of a token's codes
+  static constexpr int kSpace = (kSmall ? 8192 : 16384) * PARTS;    // codes of 8 bits: 128 KiB a CU
+  static constexpr int kTokens = kFour<T> ? (PARTS == 1 ? 32 : 64) : kSpace >= 4 * 64 * D ? 64 : 32;
+  static constexpr int kHalf = kTokens * kRow, kSlot = 2 * kHalf + (kFour<T> ? 512 : 0);  // bytes of a slot's keys; in all, with scales
+  static constexpr int kDepth = !kFour<T> ? kSpace / kSlot : D == 64 && RB == 2 ? 4 : PARTS == 4 ? 4 : 2;  // slots, a power of two
+  static constexpr int kDataCopies = 2 * kHalf / 1024 / PARTS;      // of a slot, by each of its waves
+  static constexpr int kCopies = kDataCopies + (!kFour<T> ? 0 : PARTS == 1 ? 2 : 1);
+  static constexpr int kTile = kFour<T> ? 64 * D : 0;               // 32 keys' values as bf16
+  static constexpr int kMerge = PARTS * RB * 32 * D * 4;            // what the merge of the streams puts here
+  static constexpr int kUsed = kDepth * kSlot + PARTS * kTile;
+  static constexpr int kBytes = kUsed > kMerge ? kUsed : kMerge;
+};
+
 // Workgroup = (share of the work, KV head).  A wave holds RB blocks of 32 of the K x Hq/Hkv query rows that share the KV head (row =
 // depth * group + head); PARTS waves with different rows make a stream, and the streams take a request's pages in turn.  A stream
 // has a ring of slots in LDS (a page each where the ring holds two, otherwise 32 tokens), filled by its waves some slots ahead of their
@@ -320,15 +450,15 @@ __device__ __forceinline__ T* held(T* x) {  // (as a pointer to global memory, w
 // Bound: memory (64 requests of 8192 tokens: 102 us on MI355X with 24 rows of 128 features, 5.3 TB/s), with 56 rows of 64 features
 // vector issue beside it (121 us, 4.4 TB/s: 204 instructions a slot of 32 keys and 64 rows - a quarter of it exponentials - keep the vector
 // units busy for 64 % of a wave's time, the 16 matrix instructions theirs for 34 %).
-template <int D, bool E5M2, int RB, int PARTS, int WAVES>
+template <int D, CacheType T, int RB, int PARTS, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
   constexpr int kWaves = WAVES, kStreams = kWaves / PARTS;
-  constexpr int kRing = (D == 64 && RB == 1 ? 8192 : 16384) * kWaves / kStreams;  // bytes of a stream's ring: 128 KiB a CU
-  constexpr int kTokens = kRing >= 4 * 64 * D ? 64 : 32, kHalf = kTokens * D, kSlot = 2 * kHalf;  // a slot: bytes of its keys, in all
-  constexpr int kPerPage = kKeysPerTile / kTokens, kDepth = kRing / kSlot;                        // slots of a page, of a ring
-  constexpr int kCopies = kSlot / 1024 / PARTS;                               // of a slot, by each of a stream's waves
+  using R = Ring<D, T, RB, PARTS>;
+  constexpr int kTokens = R::kTokens, kHalf = R::kHalf, kSlot = R::kSlot, kDepth = R::kDepth, kRow = R::kRow;
+  constexpr int kPerPage = kKeysPerTile / kTokens;                            // slots of a page
+  constexpr int kCopies = R::kCopies;                                         // of a slot, by each of a stream's waves
   constexpr int kAhead = PARTS == 1 ? kDepth : kDepth - 1;                    // slots on their way or in use
-  __shared__ __attribute__((aligned(16))) char ring[kStreams][kDepth][kSlot];
+  __shared__ __attribute__((aligned(16))) char ring[kStreams][R::kBytes];     // slots and, with codes of 4 bits, the waves' tiles
   __shared__ f32x4 stats[kWaves][RB * 32];  // of each wave's rows: reference, the two sums
   __shared__ int wave_bad[kWaves];
 
@@ -371,7 +501,18 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
   int c = s.c, skip = s.skip;
 
   int k_off[D / 32], v_off[D / 32];
-  {
+  Off4<D> off4;
+  char* const tile = &ring[stream][kDepth * kSlot] + part * R::kTile;
+  if constexpr (kFour<T>) {
+    off4.tr = tr_offsets<D>(lane);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      off4.codes[j] = ln * kRow + (((2 * j + g) ^ swz4<D>(ln)) << 4);
+      off4.scale[j] = ln * (D / 32) + 2 * j + g;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) off4.out[j][w] = tile_off<D>(ln, 4 * (2 * j + g) + w);
+    }
+  } else {
     const int i = lane & 15, row = 4 * g + (i >> 1 & 3) + (i >> 3) * 8;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
@@ -380,24 +521,32 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
     }
   }
   // Copies: lane l of the 1 KiB block b of a slot's half owns LDS bytes [1024 b + 16 l, + 16) and fetches the chunk that lives there.
-  constexpr int kLanes = D / 16;  // of a row
+  constexpr int kLanes = kRow / 16;  // of a row
   uint32_t voff[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
-    voff[b] = (uint32_t)((lane / kLanes) * D + ((lane % kLanes ^ swz8<D>(b * (64 / kLanes) + lane / kLanes)) << 4));
-  const uint32_t ring_at = lds_scalar_addr(&ring[stream][0][0]);
+    voff[b] = (uint32_t)((lane / kLanes) * kRow + ((lane % kLanes ^ swz_codes<D, T>(b * (64 / kLanes) + lane / kLanes)) << 4));
+  const uint32_t ring_at = lds_scalar_addr(&ring[stream][0]);
   // This wave's copies of a slot: f(values rather than keys?, block of 1 KiB).
   auto each_copy = [&](auto f) {
+    constexpr int n = R::kDataCopies;
     if constexpr (PARTS == 1) {
 #pragma unroll
-      for (int b = 0; b < kCopies / 2; ++b) f(false, b);
+      for (int b = 0; b < n / 2; ++b) f(false, b);
 #pragma unroll
-      for (int b = 0; b < kCopies / 2; ++b) f(true, b);
+      for (int b = 0; b < n / 2; ++b) f(true, b);
     } else {
-      const int b0 = part % (PARTS / 2) * kCopies;
+      const int b0 = part % (PARTS / 2) * n;
 #pragma unroll
-      for (int b = 0; b < kCopies; ++b) f(part >= PARTS / 2, b0 + b);
+      for (int b = 0; b < n; ++b) f(part >= PARTS / 2, b0 + b);
     }
+  };
+  // Scales of a slot with codes of 4 bits, a word a lane (where there are fewer than 64 words, several lanes take the same one; the
+  // waves that share the copies of K, or V, all copy its scales).
+  const uint32_t scale_off = (uint32_t)(lane * 4) % (uint32_t)(kTokens * (D / 32));
+  auto copy_scales = [&](size_t at, uint32_t dst) {
+    if (PARTS == 1 || part < PARTS / 2) dma4_untracked(uniform_ptr(k_scale + at), scale_off, dst + 2 * kHalf);
+    if (PARTS == 1 || part >= PARTS / 2) dma4_untracked(uniform_ptr(v_scale + at), scale_off, dst + 2 * kHalf + 256);
   };
 
   for (int segment = 0;;) {
@@ -428,13 +577,13 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         const int row = (part * RB + rb) * 32 + (l & 31);
         depth[rb] = row < n_rows ? small_quotient(row, p.group_reciprocal) : 0;
         const int head = kvh * p.group + (row < n_rows ? row - depth[rb] * p.group : 0);
-        const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 16 * (l >> 5);
+        const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 8 * q_chunk<T>(0, 1) * (l >> 5);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + (i / 2) * 32 + (i % 2) * 8));
+        for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + 8 * q_chunk<T>(i, 0)));
       }
     };
 
-    // The last stream's slots hold the new keys first.
+    // The last stream has the new keys first: in its first slots or, with codes of 4 bits, in its waves' tiles.
     const int n_new = has_new ? (p.K + kNewKeys - 1) / kNewKeys : 0, my_new = stream == kStreams - 1 ? n_new : 0;
     const size_t new_at = ((size_t)c * p.K * p.Hkv + kvh) * D;
     const __bf16* k_new = uniform_ptr(p.k_new + new_at);
@@ -447,7 +596,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
     int page, keys, kcode, vcode, q0, n_q, issued;
     auto copy = [&](int q) {
       const uint32_t dst = ring_at + (uint32_t)(q & (kDepth - 1)) * kSlot;
-      if (q < q0) {
+      if (!kFour<T> && q < q0) {
         const int l = lane_id();
         each_copy([&](bool half, int b) {
           const int row = b * (512 / D) + l / (D / 8), key = q * kNewKeys + row;
@@ -457,7 +606,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         return;
       }
       const int j = (q - q0) / kPerPage, sub = (q - q0) % kPerPage;
-      const size_t at = ((size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh) * (kKeysPerTile * D) + sub * kHalf;
+      const size_t page_head = (size_t)(uint32_t)__builtin_amdgcn_readlane(page, j) * p.Hkv + kvh;
+      const size_t at = page_head * (kKeysPerTile * kRow) + sub * kHalf;
+      if constexpr (kFour<T>) copy_scales((page_head * kKeysPerTile + sub * kTokens) * (D / 32), dst);
       const int present = __builtin_amdgcn_readlane(keys, j) - sub * kTokens;
       if (present >= kTokens) {
         each_copy([&](bool half, int b) {
@@ -467,7 +618,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         const int last = present > 0 ? present - 1 : 0, l = lane_id();
         each_copy([&](bool half, int b) {
           const int row = b * (64 / kLanes) + l / kLanes;
-          const uint32_t off = (uint32_t)((row < last ? row : last) * D + ((l % kLanes ^ swz8<D>(row)) << 4));
+          const uint32_t off = (uint32_t)((row < last ? row : last) * kRow + ((l % kLanes ^ swz_codes<D, T>(row)) << 4));
           dma16_untracked(uniform_ptr((half ? v_pages : k_pages) + at), off, dst + (half ? kHalf : 0) + b * 1024);
         });
       }
@@ -486,12 +637,12 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       const int keys_here = n_ctx - pi * kKeysPerTile;
       keys = !there || !fine ? 0 : keys_here < kKeysPerTile ? keys_here : kKeysPerTile;
       kcode = vcode = 0;
-      if (there) {
+      if (!kFour<T> && there) {
         kcode = k_scale[(size_t)page * p.Hkv + kvh];
         vcode = v_scale[(size_t)page * p.Hkv + kvh];
       }
       const int n_here = n_mine - first < 64 ? n_mine - first : 64;
-      q0 = n_before;
+      q0 = kFour<T> ? 0 : n_before;
       n_q = q0 + (n_here > 0 ? n_here * kPerPage : 0);
       // (one slot's copies with the loads: behind more, the wait for the loads would be one for the slots that are due later)
       issued = 0;
@@ -514,15 +665,39 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       if (issued < n_q) copy(issued++);
     };
 
+    const uint32_t tile_at = ring_at + (uint32_t)(kDepth * kSlot + part * R::kTile);
+    auto copy_new = [&](int i) {  // sixteen new keys to this wave's tile, K rows of 2 D bytes, V behind them
+      const int l = lane_id();
+#pragma unroll
+      for (int b = 0; b < D / 16; ++b) {
+        const int row = b % (D / 32) * (512 / D) + l / (D / 8), key = i * kNewKeys + row;
+        const uint32_t off = (uint32_t)(key < p.K ? key : p.K - 1) * (uint32_t)(p.Hkv * D * 2) + ((l % (D / 8) ^ swz<D>(row)) << 4);
+        dma16_untracked(b >= D / 32 ? v_new : k_new, off, tile_at + b * 1024);
+      }
+    };
+    if (kFour<T> && my_new > 0) copy_new(0);
     take_pages(0, my_new);
     int q = 0;
+    if constexpr (kFour<T>) {
+      for (int i = 0; i < my_new; ++i) {
+        if (i == 0) {
+          wait_slots<kAhead, kCopies>(issued);
+        } else {
+          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the tile's last reads have left it
+          copy_new(i);
+          wait_outstanding<0>();
+        }
+        new_keys<D, T, RB>(r, tile, tile + kNewKeys * 2 * D, i * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+      }
+      asm volatile("" : : : "memory");
+    }
     // (where streams meet at barriers, the others wait for the new keys' turns)
-    for (int i = 0; i < (PARTS > 1 ? n_new : my_new); ++i) {
+    for (int i = 0; !kFour<T> && i < (PARTS > 1 ? n_new : my_new); ++i) {
       if (my_new > 0) begin(q);
       else if (PARTS > 1) __syncthreads();
       if (my_new > 0) {
-        const char* at = ring[stream][q & (kDepth - 1)];
-        new_keys<D, RB>(r, at, at + kHalf, q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+        const char* at = &ring[stream][(q & (kDepth - 1)) * kSlot];
+        new_keys<D, T, RB>(r, at, at + kHalf, q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
         end();
         ++q;
       }
@@ -533,11 +708,18 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         const bool starts = kTokens == 32 || i % 2 == 0, ends = kTokens == 32 || i % 2 != 0;  // a slot's turn
         if (starts) begin(q);
         const int j = i / 2, n = __builtin_amdgcn_readlane(keys, j) - i % 2 * 32;  // (0 behind this stream's pages)
-        const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
-        const int v_code = __builtin_amdgcn_readlane(vcode, j);
-        const float vs = __builtin_bit_cast(float, v_code << 23), limit = v_code > kFarScale ? kNearLimit : kFarLimit;
-        const char* at = ring[stream][q & (kDepth - 1)] + (kTokens == 32 ? 0 : i % 2 * 32 * D);
-        if (n > 0) cached_keys<D, E5M2, RB>(r, at, at + kHalf, k_off, v_off, ks, vs, limit, n, g, p.c_log2);
+        const char* slot = &ring[stream][(q & (kDepth - 1)) * kSlot];
+        const int half = kTokens == 32 ? 0 : i % 2;
+        const char* at = slot + half * 32 * kRow;
+        if constexpr (kFour<T>) {
+          const char* scales = slot + 2 * kHalf + half * D;
+          if (n > 0) cached_keys4<D, RB>(r, at, at + kHalf, scales, scales + 256, tile, off4, n, ln, g, p.c_log2);
+        } else {
+          const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
+          const int v_code = __builtin_amdgcn_readlane(vcode, j);
+          const float vs = __builtin_bit_cast(float, v_code << 23), limit = v_code > kFarScale ? kNearLimit : kFarLimit;
+          if (n > 0) cached_keys<D, T, RB>(r, at, at + kHalf, k_off, v_off, ks, vs, limit, n, g, p.c_log2);
+        }
         if (ends) {
           end();
           ++q;
@@ -568,7 +750,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
     const size_t rec = ((size_t)kvh * n_groups + blockIdx.x) * 2 + (segment > 0 ? 1 : 0);
     constexpr int kRegion = RB * 32 * D / 4;
     static_assert(kWaves * kRegion * 16 <= (int)sizeof(ring), "the rows' O must fit a wave's part of the rings");
-    f32x4* regions = reinterpret_cast<f32x4*>(&ring[0][0][0]);
+    f32x4* regions = reinterpret_cast<f32x4*>(&ring[0][0]);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int at = rb * 32 + (l & 31), row = part * RB * 32 + at;
@@ -763,7 +945,7 @@ ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
   return r;
 }
 
-hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, hipStream_t stream) {
+hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, CacheType cache, hipStream_t stream) {
   ScaledDecodeParams p = pin;
   p.d.group = p.d.Hq / p.d.Hkv;
   p.d.group_reciprocal = small_reciprocal(p.d.group);
@@ -778,7 +960,7 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, 
   // against 94 us for 64 of 512 to 8192).
   const bool alone = (int64_t)grid.x * grid.y <= kCus;
   auto go = [&](auto type) {
-    constexpr bool T = decltype(type)::value;
+    constexpr CacheType T = decltype(type)::value;
     auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)waves * 64), 0, stream, p); };
     if (D == 64) {
       if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1, 8>, 8);
@@ -795,7 +977,11 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, bool e5m2, 
       else run(draft_scaled_kernel<128, T, 1, 4, 8>, 8);
     }
   };
-  e5m2 ? go(std::true_type{}) : go(std::false_type{});
+  switch (cache) {
+    case CacheType::kE4M3: go(std::integral_constant<CacheType, CacheType::kE4M3>()); break;
+    case CacheType::kE5M2: go(std::integral_constant<CacheType, CacheType::kE5M2>()); break;
+    case CacheType::kE2M1: go(std::integral_constant<CacheType, CacheType::kE2M1>()); break;
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.shares == 0) return e;
   auto merge = [&](auto kernel, int rows) {
