@@ -196,10 +196,18 @@ __device__ __forceinline__ void cached_keys(Rows<D, RB>& r, const char* k_at, co
 // are.
 template <int D>
 struct Off4 {
-  int codes[D / 64], scale[D / 64];  // of a lane's 16-byte chunk j, features 32 (2 j + g) .. + 32 of key lane % 32, and its scale
-  int out[D / 64][4];                // of its eight features w in the tile
+  int codes[D / 64], scale[D / 64];      // of a lane's 16-byte chunk j, features 32 (2 j + g) .. + 32 of key lane % 32, and its scale
+  int v_codes[D / 64], v_scale[D / 64];  // of its chunk of value_key()
+  int out[D / 64][4];                    // of that one's eight features w in the tile
   TrOff<D> tr;
 };
+// The key whose values a lane widens, of 32: eight lanes that follow each other write to eight different 16-byte places modulo 128
+// bytes of the tile (in the lanes' own order two of them share each place, which takes twice as long).
+template <int D>
+__device__ __forceinline__ int value_key(int ln) {
+  const int i = ln & 7, h = (ln >> 3) & 1;
+  return (ln & 16) | (D == 64 ? 2 * i + h : ((i >> 1) << 2) | (h << 1) | (i & 1));
+}
 template <int D, int RB>
 __device__ __forceinline__ void cached_keys4(Rows<D, RB>& r, const char* k_at, const char* v_at, const char* ks_at, const char* vs_at, char* tile,
                                              const Off4<D>& off, int n, int ln, int g, float c) {
@@ -212,16 +220,16 @@ __device__ __forceinline__ void cached_keys4(Rows<D, RB>& r, const char* k_at, c
   }
 #pragma unroll
   for (int j = 0; j < D / 64; ++j) {
-    vw[j] = *reinterpret_cast<const u32x4*>(v_at + off.codes[j]);
-    vs[j] = *reinterpret_cast<const uint8_t*>(vs_at + off.scale[j]);
+    vw[j] = *reinterpret_cast<const u32x4*>(v_at + off.v_codes[j]);
+    vs[j] = *reinterpret_cast<const uint8_t*>(vs_at + off.v_scale[j]);
   }
   __builtin_amdgcn_sched_barrier(0);
   if (n < 32) {  // (whatever stands behind the last key: zeros)
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      vs[j] = ln < n ? vs[j] : 127u;
+      vs[j] = value_key<D>(ln) < n ? vs[j] : 127u;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) vw[j][w] = ln < n ? vw[j][w] : 0u;
+      for (int w = 0; w < 4; ++w) vw[j][w] = value_key<D>(ln) < n ? vw[j][w] : 0u;
     }
   }
   bool large = false;
@@ -271,6 +279,151 @@ __device__ __forceinline__ void cached_keys4(Rows<D, RB>& r, const char* k_at, c
     }
   __builtin_amdgcn_s_setprio(0);
   asm volatile("" : : : "memory");
+}
+
+// 32 keys in stages, for a wave that has two at work: while the vector unit turns the scores of one into probabilities, the matrix
+// unit multiplies the next one's keys.
+template <int D>
+struct Keys4 {
+  u32x4 k[D / 64], v[D / 64];
+  uint32_t ks[D / 64], vs[D / 64];
+};
+template <int D>
+__device__ __forceinline__ void load4(Keys4<D>& x, const char* k_at, const char* v_at, const char* ks_at, const char* vs_at, const Off4<D>& off) {
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    x.k[j] = *reinterpret_cast<const u32x4*>(k_at + off.codes[j]);
+    x.ks[j] = *reinterpret_cast<const uint8_t*>(ks_at + off.scale[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    x.v[j] = *reinterpret_cast<const u32x4*>(v_at + off.v_codes[j]);
+    x.vs[j] = *reinterpret_cast<const uint8_t*>(vs_at + off.v_scale[j]);
+  }
+}
+template <int D>
+__device__ __forceinline__ bf16x8 key_features(const Keys4<D>& x, int i) {  // of step i of the product with the queries
+  const uint32_t word = x.k[i / 4][i % 4];
+  return widen4(word, __builtin_bit_cast(float, x.ks[i / 4] << 23));
+}
+template <int D, int RB>
+__device__ __forceinline__ void scores4(const Keys4<D>& x, const Rows<D, RB>& r, f32x16 (&s)[RB]) {
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const bf16x8 a = key_features(x, i);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) s[rb] = mfma32(a, r.q[rb][i], i == 0 ? zero16() : s[rb]);
+  }
+}
+// The values to the tile, zeros from key n on.  Returns the limit that goes with their scales.
+template <int D>
+__device__ __forceinline__ float values4(Keys4<D>& x, char* tile, const Off4<D>& off, int n, int ln) {
+  if (n < 32) {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      x.vs[j] = value_key<D>(ln) < n ? x.vs[j] : 127u;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) x.v[j][w] = value_key<D>(ln) < n ? x.v[j][w] : 0u;
+    }
+  }
+  bool large = false;
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    large |= x.vs[j] > (uint32_t)kFarScale && x.vs[j] != 255u;  // (NaN changes no bit of other features)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t word = x.v[j][w];
+      *reinterpret_cast<bf16x8*>(tile + off.out[j][w]) = widen4(word, __builtin_bit_cast(float, x.vs[j] << 23));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  return __builtin_amdgcn_ballot_w64(large) != 0 ? kNearLimit : kFarLimit;
+}
+// One turn: what the scores s of n keys weigh in the output, their values being in the tile; the next keys' scores.  Every matrix
+// instruction is followed by its share of the vector instructions, and by a fence so that this order stays.  With two blocks of rows
+// the second one's product with the values waits for the next turn (`Held4`), so that fewer registers hold what is in between.
+template <int D>
+struct Held4 {
+  bf16x8 v[2][D / 32], p[2];
+};
+template <int D, int RB>
+__device__ __forceinline__ void take4(Rows<D, RB>& r, f32x16 (&s)[RB], f32x16 (&s_next)[RB], const Keys4<D>& next, Held4<D>& held, const char* tile,
+                                      const Off4<D>& off, int n, float limit, int g, float c) {
+  static_assert(RB <= 2, "");
+  constexpr int kSteps = D / 16, kFrags = D / 32;
+  auto load_values = [&](int t) {
+#pragma unroll
+    for (int db = 0; db < kFrags; ++db) held.v[t][db] = frag_tr<D>(tile, off.tr, 16 * t, db);
+  };
+  if (n < 32) {
+    const uint32_t bits = n <= 0 ? 0u : ((1u << n) - 1) >> (4 * g);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[rb][i] = mask_sel(s[rb][i], bits, 8 * (i / 4) + (i % 4));
+  }
+  f32x16 x;
+  float sum[4];
+  auto weigh = [&](int rb, int from, int to) {
+#pragma unroll
+    for (int i = from; i < to; ++i) {
+      x[i] = exp2_fast(__builtin_fmaf(s[rb][i], c, -r.m[rb]));
+      sum[i % 4] = i < 4 ? x[i] : sum[i % 4] + x[i];
+    }
+  };
+  auto check = [&](int rb) {
+    float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(total > limit) != 0, 0)) {
+      const float mx = max_halves(max16(s[rb])) * c;
+      const bool need = max_halves(total) > limit && mx > r.m[rb];
+      const float m_new = need ? mx : r.m[rb], alpha = exp2_fast(r.m[rb] - m_new);
+      r.m[rb] = m_new;
+      r.l[rb] *= alpha;
+      r.w[rb] *= alpha;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r.o[rb][db][i] *= alpha;
+      weigh(rb, 0, 16);
+      total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+    r.l[rb] += total;
+    held.p[0] = pack8_sum(x, 0, r.w[rb]);
+    held.p[1] = pack8_sum(x, 1, r.w[rb]);
+  };
+  auto weigh_value = [&](int rb, int k) { r.o[rb][k % kFrags] = mfma32(held.v[k / kFrags][k % kFrags], held.p[k / kFrags], r.o[rb][k % kFrags]); };
+  if constexpr (RB == 2) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < 2 * kFrags; ++k) {
+      weigh_value(1, k);
+      weigh(0, 16 * k / (2 * kFrags), 16 * (k + 1) / (2 * kFrags));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    check(0);
+    load_values(0);
+    load_values(1);
+  }
+  constexpr int kNext = RB * kSteps, kMatrix = kNext + (RB == 2 ? 2 * kFrags : 0);
+  __builtin_amdgcn_sched_barrier(0);
+  bf16x8 a = key_features(next, 0);
+#pragma unroll
+  for (int k = 0; k < kMatrix; ++k) {
+    if (k < kNext) s_next[k % RB] = mfma32(a, r.q[k % RB][k / RB], k < RB ? zero16() : s_next[k % RB]);
+    else weigh_value(0, k - kNext);
+    weigh(RB - 1, 16 * k / kMatrix, 16 * (k + 1) / kMatrix);
+    if (k % RB == RB - 1 && k + 1 < kNext) a = key_features(next, (k + 1) / RB);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (RB == 1) load_values(0);
+  check(RB - 1);
+  __builtin_amdgcn_sched_barrier(0);
+  if constexpr (RB == 1) {
+    load_values(1);
+#pragma unroll
+    for (int k = 0; k < 2 * kFrags; ++k) weigh_value(0, k);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 // Sixteen of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
@@ -430,11 +583,12 @@ struct Ring {
   static constexpr bool kSmall = D == 64 && RB == 1;                // four waves a SIMD, otherwise two
   static constexpr int kRow = kFour<T> ? D / 2 : D;                 // bytes of a token's codes
   static constexpr int kSpace = (kSmall ? 8192 : 16384) * PARTS;    // codes of 8 bits: 128 KiB a CU
-  static constexpr int kTokens = kFour<T> ? (PARTS == 1 ? 32 : 64) : kSpace >= 4 * 64 * D ? 64 : 32;
-  static constexpr int kHalf = kTokens * kRow, kSlot = 2 * kHalf + (kFour<T> ? 512 : 0);  // bytes of a slot's keys; in all, with scales
-  static constexpr int kDepth = !kFour<T> ? kSpace / kSlot : D == 64 && RB == 2 ? 4 : PARTS == 4 ? 4 : 2;  // slots, a power of two
+  static constexpr bool kPiped = kFour<T> && !kSmall && !(D == 128 && PARTS == 1);
+  static constexpr int kTokens = kFour<T> ? (PARTS == 1 && !kPiped ? 32 : 64) : kSpace >= 4 * 64 * D ? 64 : 32;
+  static constexpr int kHalf = kTokens * kRow, kSlot = 2 * kHalf + (kFour<T> ? (kTokens * D / 32 > 128 ? 512 : 256) : 0);  // bytes of a slot's keys; in all, with scales
+  static constexpr int kDepth = !kFour<T> ? kSpace / kSlot : PARTS == 4 ? 4 : D == 64 && RB == 2 ? 2 * PARTS : 2;  // slots
   static constexpr int kDataCopies = 2 * kHalf / 1024 / PARTS;      // of a slot, by each of its waves
-  static constexpr int kCopies = kDataCopies + (!kFour<T> ? 0 : PARTS == 1 ? 2 : 1);
+  static constexpr int kCopies = kDataCopies + (!kFour<T> ? 0 : kTokens * D / 32 > 128 && PARTS == 1 ? 2 : 1);
   static constexpr int kTile = kFour<T> ? 64 * D : 0;               // 32 keys' values as bf16
   static constexpr int kMerge = PARTS * RB * 32 * D * 4;            // what the merge of the streams puts here
   static constexpr int kUsed = kDepth * kSlot + PARTS * kTile;
@@ -507,10 +661,13 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
     off4.tr = tr_offsets<D>(lane);
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
+      const int vl = value_key<D>(ln);
       off4.codes[j] = ln * kRow + (((2 * j + g) ^ swz4<D>(ln)) << 4);
       off4.scale[j] = ln * (D / 32) + 2 * j + g;
+      off4.v_codes[j] = vl * kRow + (((2 * j + g) ^ swz4<D>(vl)) << 4);
+      off4.v_scale[j] = vl * (D / 32) + 2 * j + g;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) off4.out[j][w] = tile_off<D>(ln, 4 * (2 * j + g) + w);
+      for (int w = 0; w < 4; ++w) off4.out[j][w] = tile_off<D>(vl, 4 * (2 * j + g) + w);
     }
   } else {
     const int i = lane & 15, row = 4 * g + (i >> 1 & 3) + (i >> 3) * 8;
@@ -541,12 +698,19 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       for (int b = 0; b < n; ++b) f(part >= PARTS / 2, b0 + b);
     }
   };
-  // Scales of a slot with codes of 4 bits, a word a lane (where there are fewer than 64 words, several lanes take the same one; the
-  // waves that share the copies of K, or V, all copy its scales).
-  const uint32_t scale_off = (uint32_t)(lane * 4) % (uint32_t)(kTokens * (D / 32));
+  // Scales of a slot with codes of 4 bits, a word a lane: those of K and behind them those of V by one copy where they are 64 words or
+  // fewer (every wave of a stream makes it, the same), otherwise by two, of which the waves that copy K make one.
+  constexpr int kScaleWords = kTokens * (D / 32) / 4;
+  const uint8_t* scale_at = nullptr;
+  if constexpr (kFour<T>) scale_at = (kScaleWords <= 32 && lane / kScaleWords % 2 != 0 ? v_scale : k_scale) + lane % kScaleWords * 4;
   auto copy_scales = [&](size_t at, uint32_t dst) {
-    if (PARTS == 1 || part < PARTS / 2) dma4_untracked(uniform_ptr(k_scale + at), scale_off, dst + 2 * kHalf);
-    if (PARTS == 1 || part >= PARTS / 2) dma4_untracked(uniform_ptr(v_scale + at), scale_off, dst + 2 * kHalf + 256);
+    if constexpr (kScaleWords <= 32) {
+      dma4_untracked(scale_at + at, dst + 2 * kHalf);
+    } else {
+      const uint32_t off = (uint32_t)lane_id() * 4;
+      if (PARTS == 1 || part < PARTS / 2) dma4_untracked(uniform_ptr(k_scale + at), off, dst + 2 * kHalf);
+      if (PARTS == 1 || part >= PARTS / 2) dma4_untracked(uniform_ptr(v_scale + at), off, dst + 2 * kHalf + 4 * kScaleWords);
+    }
   };
 
   for (int segment = 0;;) {
@@ -595,7 +759,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
     // copies are begun: slots [0, q0) hold new keys, n_q slots in all.
     int page, keys, kcode, vcode, q0, n_q, issued;
     auto copy = [&](int q) {
-      const uint32_t dst = ring_at + (uint32_t)(q & (kDepth - 1)) * kSlot;
+      const uint32_t dst = ring_at + (uint32_t)q % kDepth * kSlot;
       if (!kFour<T> && q < q0) {
         const int l = lane_id();
         each_copy([&](bool half, int b) {
@@ -653,7 +817,12 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
     // A slot's turn: what it holds has landed; with several waves a stream, everyone is done with the slot before it, which is
     // filled again.
     auto begin = [&](int q) {
-      wait_slots<kAhead - 1, kCopies>(issued - 1 - q);
+      if constexpr (R::kPiped) {  // (fewer than kAhead - 1 slots behind this one are only its last ones)
+        if (issued - 1 - q >= kAhead - 1) wait_outstanding<(kAhead - 1) * kCopies>();
+        else wait_outstanding<0>();
+      } else {
+        wait_slots<kAhead - 1, kCopies>(issued - 1 - q);
+      }
       if (PARTS > 1) {
         __syncthreads();
         if (issued < n_q) copy(issued++);
@@ -696,24 +865,72 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       if (my_new > 0) begin(q);
       else if (PARTS > 1) __syncthreads();
       if (my_new > 0) {
-        const char* at = &ring[stream][(q & (kDepth - 1)) * kSlot];
+        const char* at = &ring[stream][(uint32_t)q % kDepth * kSlot];
         new_keys<D, T, RB>(r, at, at + kHalf, q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
         end();
         ++q;
       }
     }
     for (int first = 0;;) {
+      if constexpr (R::kPiped) {
+        // A slot is a page, a page two turns.  Its second half is read when the first one's turn begins, and its slot filled again
+        // when that has arrived.
+        static_assert(kTokens == 64, "");
+        const int n = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) : n_q;
+        Keys4<D> x;
+        auto load = [&](int j, int half) {
+          const char* slot = &ring[stream][(uint32_t)j % kDepth * kSlot];
+          const char* scales = slot + 2 * kHalf + half * D;
+          load4(x, slot + half * 32 * kRow, slot + kHalf + half * 32 * kRow, scales, scales + 4 * kScaleWords, off4);
+        };
+        f32x16 sa[RB], sb[RB];
+        Held4<D> held{};
+        float limit_a = kFarLimit, limit_b = kFarLimit;
+        if (n > 0) {
+          int keys_here = __builtin_amdgcn_readlane(keys, 0);
+          begin(0);
+          load(0, 0);
+          scores4(x, r, sa);
+          limit_a = values4(x, tile, off4, keys_here, ln);
+          load(0, 1);
+          // (the last turn's next keys are such as have been before, and count nowhere)
+          for (int j = 0; j < n; ++j) {
+            take4<D, RB>(r, sa, sb, x, held, tile, off4, keys_here, limit_a, g, p.c_log2);
+            limit_b = values4(x, tile, off4, keys_here - 32, ln);
+            end();
+            const int keys_next = __builtin_amdgcn_readlane(keys, j + 1);
+            if (j + 1 < n) {
+              begin(j + 1);
+              load(j + 1, 0);
+            }
+            take4<D, RB>(r, sb, sa, x, held, tile, off4, keys_here - 32, limit_b, g, p.c_log2);
+            limit_a = values4(x, tile, off4, keys_next, ln);
+            if (j + 1 < n) load(j + 1, 1);
+            keys_here = keys_next;
+          }
+          if (RB == 2) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) r.o[RB - 1][k % (D / 32)] = mfma32(held.v[k / (D / 32)][k % (D / 32)], held.p[k / (D / 32)], r.o[RB - 1][k % (D / 32)]);
+          }
+        }
+        if (PARTS > 1) __syncthreads();  // (the slots' last reads have left them)
+        first += 64;
+        if (first >= n_pages_0) break;
+        take_pages(first, 0);
+        q = 0;
+        continue;
+      }
       const int rounds = PARTS > 1 ? (n_pages_0 - first < 64 ? n_pages_0 - first : 64) * 2 : (n_q - q0) * (kTokens / 32);
       for (int i = 0; i < rounds; ++i) {
         const bool starts = kTokens == 32 || i % 2 == 0, ends = kTokens == 32 || i % 2 != 0;  // a slot's turn
         if (starts) begin(q);
         const int j = i / 2, n = __builtin_amdgcn_readlane(keys, j) - i % 2 * 32;  // (0 behind this stream's pages)
-        const char* slot = &ring[stream][(q & (kDepth - 1)) * kSlot];
+        const char* slot = &ring[stream][(uint32_t)q % kDepth * kSlot];
         const int half = kTokens == 32 ? 0 : i % 2;
         const char* at = slot + half * 32 * kRow;
         if constexpr (kFour<T>) {
           const char* scales = slot + 2 * kHalf + half * D;
-          if (n > 0) cached_keys4<D, RB>(r, at, at + kHalf, scales, scales + 256, tile, off4, n, ln, g, p.c_log2);
+          if (n > 0) cached_keys4<D, RB>(r, at, at + kHalf, scales, scales + 4 * kScaleWords, tile, off4, n, ln, g, p.c_log2);
         } else {
           const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(kcode, j) << 23);
           const int v_code = __builtin_amdgcn_readlane(vcode, j);
