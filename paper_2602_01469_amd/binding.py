@@ -10,6 +10,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libpeagle_attn.so"
 _lib = None
+_marshal = None
 
 
 class PeagleError(RuntimeError):
@@ -744,6 +745,24 @@ def peagle_draft_decode_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages,
         raise PeagleError(rc, "peagle_draft_decode_scaled")
 
 
+def _fast():
+    """The compiled part of the binding: its functions make a call whose arguments are all as they have to be and return the
+    status; of any other call they return None, and the checks here say what is wrong (or make it)."""
+    global _marshal
+    if _marshal is None:
+        import torch  # noqa: F401  (whose libraries it needs)
+        lib = load_library()
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise ImportError("_marshal.so is missing: build it with `python -m paper_2602_01469_amd.build` (or "
+                              "__graft_entry__.build())") from e
+        m.bind(*(C.cast(f, C.c_void_p).value for f in (lib.peagle_cache_append_block_scaled, lib.peagle_cache_read,
+                                                       lib.peagle_draft_decode_block_scaled)))
+        _marshal = m
+    return _marshal
+
+
 def _block_pools(device, k_pages, v_pages, k_scale, v_scale, n_pages: int, Hkv: int, D: int):
     """The pointers of a 4-bit cache's pools and scales."""
     import torch
@@ -757,6 +776,11 @@ def peagle_cache_append_block_scaled(shape: CacheShape, k_new, v_new, slots, k_p
     """Stores k_new, v_new [n_tokens, Hkv, D] (a token's heads contiguous, tokens any multiple of 8 elements apart) at `slots` of a
     4-bit cache: pools of torch.float4_e2m1fn_x2 [n_pages, Hkv, 64, D / 2], scales of torch.float8_e8m0fnu [n_pages, Hkv, 64,
     D / 32]."""
+    rc = (_marshal or _fast()).cache_append(shape, k_new, v_new, slots, k_pages, v_pages, k_scale, v_scale, stream)
+    if rc == 0:
+        return
+    if rc is not None:
+        raise PeagleError(rc, "peagle_cache_append_block_scaled")
     import torch
     s, dev = shape, k_pages.get_device()
     pools = _block_pools(dev, k_pages, v_pages, k_scale, v_scale, s.n_pages, s.Hkv, s.D)
@@ -773,6 +797,11 @@ def peagle_cache_append_block_scaled(shape: CacheShape, k_new, v_new, slots, k_p
 def peagle_cache_read(shape: CacheShape, slots, k_pages, v_pages, k_scale, v_scale, k_out, v_out, stream=None) -> None:
     """The tokens at `slots` of an 8-bit or 4-bit cache as bf16 rows k_out, v_out [n_tokens, Hkv, D] (which may stand apart as
     those of an append may); zeros for slots outside the pools."""
+    rc = (_marshal or _fast()).cache_read(shape, slots, k_pages, v_pages, k_scale, v_scale, k_out, v_out, stream)
+    if rc == 0:
+        return
+    if rc is not None:
+        raise PeagleError(rc, "peagle_cache_read")
     import torch
     s, dev = shape, k_pages.get_device()
     if k_pages.dtype is torch.float4_e2m1fn_x2:
@@ -799,6 +828,12 @@ def peagle_draft_decode_block_scaled_workspace_bytes(shape: DecodeShape) -> int:
 def peagle_draft_decode_block_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages, v_pages, k_scale, v_scale, block_table, ctx_len,
                                      o, lse, status, workspace, stream=None) -> None:
     """peagle_draft_decode on a cache held in 4 bits, as peagle_cache_append_block_scaled stores it."""
+    rc = (_marshal or _fast()).draft_decode(shape, q_new, k_new, v_new, k_pages, v_pages, k_scale, v_scale, block_table, ctx_len, o, lse,
+                                            status, workspace, stream)
+    if rc == 0:
+        return
+    if rc is not None:
+        raise PeagleError(rc, "peagle_draft_decode_block_scaled")
     import torch
     bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
     s = shape

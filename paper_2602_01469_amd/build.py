@@ -1,9 +1,11 @@
-"""Builds the HIP extension in-tree: paper_2602_01469_amd/libpeagle_attn.so (gfx950 only)."""
+"""Builds the HIP extension in-tree, paper_2602_01469_amd/libpeagle_attn.so (gfx950 only), and the binding's compiled part,
+paper_2602_01469_amd/_marshal.so (host code against the installed torch)."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -12,6 +14,25 @@ LIB = os.path.join(HERE, "libpeagle_attn.so")
 SOURCES = ["tilemap.cpp", "api.cpp", "attn_kernels.hip", "rope_kernels.hip", "cache_kernels.hip",
            "draft_scaled_kernels.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+MARSHAL = os.path.join(HERE, "_marshal.so")
+
+
+def _run(cmd, what: str) -> str:
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    out = "\n".join(l for l in r.stdout.splitlines() if "not a recognized feature" not in l)
+    if r.returncode != 0:
+        raise RuntimeError(what + " failed:\n" + out)
+    return out
+
+
+def build_marshal() -> str:
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I" + os.path.join(torch_dir, "include"),
+          "-I" + os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "-I/opt/rocm/include",
+          "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL, "-L" + os.path.join(torch_dir, "lib"),
+          "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"], "g++")
+    return MARSHAL
 
 
 def build(verbose: bool = False, sanitize_host_to: str = "") -> str:
@@ -35,10 +56,9 @@ def build(verbose: bool = False, sanitize_host_to: str = "") -> str:
     ] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Rpass-analysis=kernel-resource-usage")
-    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in r.stdout.splitlines() if "not a recognized feature" not in l)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
+    out = _run(cmd, "hipcc")
+    if not sanitize_host_to:
+        build_marshal()
     if verbose and out:
         print(out)
     return out_path
