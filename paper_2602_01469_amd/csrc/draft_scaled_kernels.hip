@@ -70,10 +70,11 @@ __device__ __forceinline__ int swz_codes(int row) {
 }
 
 // Which eight features step i of the product with the keys takes in lanes of half g: those that follow each other in a 16-byte read
-// of the keys' codes, two steps' with codes of 8 bits, four steps' with codes of 4 bits (which so have one scale).
-template <CacheType T>
+// of the keys' codes, two steps' with codes of 8 bits, four steps' with codes of 4 bits (which so have one scale).  SHARED: the keys
+// are read as bf16.
+template <CacheType T, bool SHARED = false>
 __device__ __forceinline__ int q_chunk(int i, int g) {
-  return kFour<T> ? 8 * (i / 4) + 4 * g + i % 4 : 4 * (i / 2) + 2 * g + i % 2;
+  return SHARED ? 2 * i + g : kFour<T> ? 8 * (i / 4) + 4 * g + i % 4 : 4 * (i / 2) + 2 * g + i % 2;
 }
 
 // State of RB blocks of 32 query rows: lane <-> row, registers <-> features 32 db + 8 (i / 4) + 4 g + i % 4.
@@ -426,19 +427,80 @@ __device__ __forceinline__ void take4(Rows<D, RB>& r, f32x16 (&s)[RB], f32x16 (&
   }
 }
 
+// Several waves with different rows: each widens its share of 32 keys, and all of them read them as bf16 rows of two tiles of keys and
+// two of values, one of each being written while the other is read.
+template <int PARTS>
+struct Raw4 {  // a lane's share at D = 128: features of one key and block, and their scale
+  uint32_t w[8 / PARTS], scale;
+};
+template <int PARTS>
+struct Share4 {
+  int key, codes, scale;  // which key of 32; offsets of its codes and its scale
+  int out;                // place of its first eight features in a tile
+  __device__ __forceinline__ Share4(int part, int lane) {
+    constexpr int D = 128;
+    const int i = lane & 7, block = PARTS == 2 ? lane >> 4 : (lane >> 3) & 3, half = PARTS == 2 ? 0 : lane >> 5;
+    // (eight lanes that follow each other write to eight places modulo 128 bytes, as in value_key())
+    const int h = PARTS == 2 ? (lane >> 3) & 1 : part & 1;
+    key = (PARTS == 2 ? part : part >> 1) * 16 + (((i >> 1) << 2) | (h << 1) | (i & 1));
+    codes = key * (D / 2) + block * 16 + half * 8;
+    scale = key * (D / 32) + block;
+    out = tile_off<D>(key, 4 * block + 2 * half);
+  }
+};
+// (as global memory: a load that might be from LDS would be waited for with the LDS reads)
+template <class V>
+__device__ __forceinline__ V load_global(const uint8_t* base, uint32_t off) {
+  typedef const __attribute__((address_space(1))) uint8_t bytes;
+  return *(const __attribute__((address_space(1))) V*)((bytes*)base + off);
+}
+template <int PARTS>
+__device__ __forceinline__ void load_share(Raw4<PARTS>& x, const uint8_t* codes, const uint8_t* scales, const Share4<PARTS>& mine) {
+  if constexpr (PARTS == 2) {
+    const u32x4 w = load_global<u32x4>(codes, (uint32_t)mine.codes);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.w[i] = w[i];
+  } else {
+    const u32x2 w = load_global<u32x2>(codes, (uint32_t)mine.codes);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x.w[i] = w[i];
+  }
+  x.scale = load_global<uint8_t>(scales, (uint32_t)mine.scale);
+}
+template <int PARTS>
+__device__ __forceinline__ void put_share(const Raw4<PARTS>& x, char* tile, const Share4<PARTS>& mine, int i) {  // its eight features i
+  *reinterpret_cast<bf16x8*>(tile + (mine.out ^ (i << 4))) = widen4(x.w[i], __builtin_bit_cast(float, x.scale << 23));
+}
+template <int PARTS>
+__device__ __forceinline__ void keep_first(Raw4<PARTS>& x, const Share4<PARTS>& mine, int n) {  // zeros from key n on
+  if (n < 32) {
+    x.scale = mine.key < n ? x.scale : 127u;
+#pragma unroll
+    for (int i = 0; i < 8 / PARTS; ++i) x.w[i] = mine.key < n ? x.w[i] : 0u;
+  }
+}
+template <int PARTS>
+__device__ __forceinline__ bool far_scale(const Raw4<PARTS>& x) {
+  return __builtin_amdgcn_ballot_w64(x.scale > (uint32_t)kFarScale && x.scale != 255u) != 0;
+}
+// LDS of a workgroup whose waves share: all that it has written is there, and what it has read need not be any more.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
 // Sixteen of the request's new keys (bf16, staged in a slot: K rows of 2 D bytes, V behind them, in the layout of the bf16 tiles),
 // the first of them key k0; the row of depth d sees keys 0..d.  A masked key weighs zero, and zero times an infinity or NaN is
 // NaN: such values are taken out of the product and added to the rows that see them, from v_new (key 0 of the KV head, the next
 // one `stride` elements on).
 constexpr int kNewKeys = 16;
-template <int D, CacheType T, int RB>
+template <int D, CacheType T, int RB, bool SHARED>
 __device__ __forceinline__ void new_keys(Rows<D, RB>& r, const char* k_at, const char* v_at, int k0, int K, const __bf16* v_new, uint32_t stride,
                                          const int (&depth)[RB], float c) {
   const int lane = lane_id(), g = lane >> 5, row = lane % kNewKeys;
   bf16x8 ka[D / 16], va[D / 32];
   const TrOff<D> to = tr_offsets<D>(lane);
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(k_at + tile_off<D>(row, q_chunk<T>(i, g)));
+  for (int i = 0; i < D / 16; ++i) ka[i] = *reinterpret_cast<const bf16x8*>(k_at + tile_off<D>(row, q_chunk<T, SHARED>(i, g)));
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) va[db] = frag_tr<D>(v_at, to, 0, db);
   __builtin_amdgcn_sched_barrier(0);
@@ -583,15 +645,16 @@ struct Ring {
   static constexpr bool kSmall = D == 64 && RB == 1;                // four waves a SIMD, otherwise two
   static constexpr int kRow = kFour<T> ? D / 2 : D;                 // bytes of a token's codes
   static constexpr int kSpace = (kSmall ? 8192 : 16384) * PARTS;    // codes of 8 bits: 128 KiB a CU
-  static constexpr bool kPiped = kFour<T> && !kSmall && !(D == 128 && PARTS == 1);
+  static constexpr bool kShared = kFour<T> && D == 128 && PARTS == 4;  // waves with different rows widen each key once between them
+  static constexpr bool kPiped = kFour<T> && !kSmall && !kShared && !(D == 128 && PARTS == 1);
   static constexpr int kTokens = kFour<T> ? (PARTS == 1 && !kPiped ? 32 : 64) : kSpace >= 4 * 64 * D ? 64 : 32;
   static constexpr int kHalf = kTokens * kRow, kSlot = 2 * kHalf + (kFour<T> ? (kTokens * D / 32 > 128 ? 512 : 256) : 0);  // bytes of a slot's keys; in all, with scales
-  static constexpr int kDepth = !kFour<T> ? kSpace / kSlot : PARTS == 4 ? 4 : D == 64 && RB == 2 ? 2 * PARTS : 2;  // slots
+  static constexpr int kDepth = !kFour<T> ? kSpace / kSlot : D == 64 && RB == 2 ? 2 * PARTS : 2;  // slots
   static constexpr int kDataCopies = 2 * kHalf / 1024 / PARTS;      // of a slot, by each of its waves
   static constexpr int kCopies = kDataCopies + (!kFour<T> ? 0 : kTokens * D / 32 > 128 && PARTS == 1 ? 2 : 1);
   static constexpr int kTile = kFour<T> ? 64 * D : 0;               // 32 keys' values as bf16
   static constexpr int kMerge = PARTS * RB * 32 * D * 4;            // what the merge of the streams puts here
-  static constexpr int kUsed = kDepth * kSlot + PARTS * kTile;
+  static constexpr int kUsed = kShared ? 4 * kTile : kDepth * kSlot + PARTS * kTile;
   static constexpr int kBytes = kUsed > kMerge ? kUsed : kMerge;
 };
 
@@ -614,6 +677,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
   constexpr int kAhead = PARTS == 1 ? kDepth : kDepth - 1;                    // slots on their way or in use
   __shared__ __attribute__((aligned(16))) char ring[kStreams][R::kBytes];     // slots and, with codes of 4 bits, the waves' tiles
   __shared__ f32x4 stats[kWaves][RB * 32];  // of each wave's rows: reference, the two sums
+  __shared__ int far[kStreams][2][PARTS];   // a wave's share of the values in either tile has large scales
   __shared__ int wave_bad[kWaves];
 
   DecodeParams p = sp.d;
@@ -656,7 +720,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
 
   int k_off[D / 32], v_off[D / 32];
   Off4<D> off4;
-  char* const tile = &ring[stream][kDepth * kSlot] + part * R::kTile;
+  char* const tile = &ring[stream][R::kShared ? 0 : kDepth * kSlot] + part * R::kTile;
   if constexpr (kFour<T>) {
     off4.tr = tr_offsets<D>(lane);
 #pragma unroll
@@ -741,9 +805,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
         const int row = (part * RB + rb) * 32 + (l & 31);
         depth[rb] = row < n_rows ? small_quotient(row, p.group_reciprocal) : 0;
         const int head = kvh * p.group + (row < n_rows ? row - depth[rb] * p.group : 0);
-        const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 8 * q_chunk<T>(0, 1) * (l >> 5);
+        const __bf16* q = p.q_new + (((size_t)c * p.K + depth[rb]) * p.Hq + head) * D + 8 * q_chunk<T, R::kShared>(0, 1) * (l >> 5);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + 8 * q_chunk<T>(i, 0)));
+        for (int i = 0; i < D / 16; ++i) r.q[rb][i] = as_frag(ld16(q + 8 * q_chunk<T, R::kShared>(i, 0)));
       }
     };
 
@@ -807,7 +871,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       }
       const int n_here = n_mine - first < 64 ? n_mine - first : 64;
       q0 = kFour<T> ? 0 : n_before;
-      n_q = q0 + (n_here > 0 ? n_here * kPerPage : 0);
+      n_q = R::kShared ? 0 : q0 + (n_here > 0 ? n_here * kPerPage : 0);  // (none where waves load their shares)
       // (one slot's copies with the loads: behind more, the wait for the loads would be one for the slots that are due later)
       issued = 0;
       if (n_q > 0) copy(issued++);
@@ -834,7 +898,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       if (issued < n_q) copy(issued++);
     };
 
-    const uint32_t tile_at = ring_at + (uint32_t)(kDepth * kSlot + part * R::kTile);
+    const uint32_t tile_at = ring_at + (uint32_t)((R::kShared ? 0 : kDepth * kSlot) + part * R::kTile);
     auto copy_new = [&](int i) {  // sixteen new keys to this wave's tile, K rows of 2 D bytes, V behind them
       const int l = lane_id();
 #pragma unroll
@@ -856,7 +920,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
           copy_new(i);
           wait_outstanding<0>();
         }
-        new_keys<D, T, RB>(r, tile, tile + kNewKeys * 2 * D, i * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+        new_keys<D, T, RB, R::kShared>(r, tile, tile + kNewKeys * 2 * D, i * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
       }
       asm volatile("" : : : "memory");
     }
@@ -866,12 +930,145 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
       else if (PARTS > 1) __syncthreads();
       if (my_new > 0) {
         const char* at = &ring[stream][(uint32_t)q % kDepth * kSlot];
-        new_keys<D, T, RB>(r, at, at + kHalf, q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
+        new_keys<D, T, RB, false>(r, at, at + kHalf, q * kNewKeys, p.K, v_new, (uint32_t)(p.Hkv * D), depth, p.c_log2);
         end();
         ++q;
       }
     }
     for (int first = 0;;) {
+      if constexpr (R::kShared) {
+        const int n = n_pages_0 - first < 64 ? n_pages_0 - first : 64;
+        const Share4<PARTS> mine(part, lane_id());
+        const NatOff<D> nat = nat_offsets<D>(lane_id());
+        char* const tiles = &ring[stream][0];
+        auto k_tile = [&](int b) { return tiles + b * R::kTile; };
+        auto v_tile = [&](int b) { return tiles + (2 + b) * R::kTile; };
+        auto load = [&](Raw4<PARTS>& x, int u, const uint8_t* pages, const uint8_t* scales) {  // of 32 keys u
+          u = u < 2 * n ? u : u % 2;  // (always a load, so that what is under way can be counted)
+          const size_t page_head = (size_t)(uint32_t)__builtin_amdgcn_readlane(page, u / 2) * p.Hkv + kvh;
+          load_share(x, uniform_ptr(pages + page_head * (64 * kRow) + u % 2 * (32 * kRow)),
+                     uniform_ptr(scales + page_head * (2 * D) + u % 2 * D), mine);
+        };
+        auto keys_of = [&](int u) { return __builtin_amdgcn_readlane(keys, u / 2) - u % 2 * 32; };
+        auto put = [&](const Raw4<PARTS>& x, char* to) {
+#pragma unroll
+          for (int i = 0; i < 8 / PARTS; ++i) put_share(x, to, mine, i);
+        };
+        auto put_values = [&](Raw4<PARTS>& x, int u, int b) {
+          keep_first(x, mine, keys_of(u));
+          const int large = far_scale(x);
+          put(x, v_tile(b));
+          if (lane == 0) far[stream][b][part] = large;
+        };
+        if (n > 0) {
+          Raw4<PARTS> kr[2], vr[2];
+          load(kr[0], 0, k_pages, k_scale);
+          load(vr[0], 0, v_pages, v_scale);
+          load(kr[1], 1, k_pages, k_scale);
+          load(vr[1], 1, v_pages, v_scale);
+          meet();  // (new keys, and what was here before, have been read)
+          put(kr[0], k_tile(0));
+          put_values(vr[0], 0, 0);
+          put(kr[1], k_tile(1));
+          load(kr[0], 2, k_pages, k_scale);
+          load(kr[1], 3, k_pages, k_scale);
+          load(vr[0], 2, v_pages, v_scale);
+          meet();
+          f32x16 sa, sb;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) sa = mfma32(frag_nat<D>(k_tile(0), nat, 0, i), r.q[0][i], i == 0 ? zero16() : sa);
+          // One turn: keys u weigh the output, the scores of keys u + 1 are formed, keys u + 2 and the values of keys u + 1 widened.
+          // What is behind the last keys is what has been before, and counts nowhere.
+          auto turn = [&](auto b_, int u, f32x16& s, f32x16& s_next) {
+            constexpr int b = decltype(b_)::value, kSteps = D / 16, kFrags = D / 32;
+            meet();
+            int any_far = 0;
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) any_far |= far[stream][b][i];
+            bf16x8 kf[2], vf[2][kFrags];
+            kf[0] = frag_nat<D>(k_tile(1 - b), nat, 0, 0);
+            kf[1] = frag_nat<D>(k_tile(1 - b), nat, 0, 1);
+            const int n_keys = keys_of(u);
+            if (n_keys < 32) {
+              const uint32_t bits = n_keys <= 0 ? 0u : ((1u << n_keys) - 1) >> (4 * g);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) s[i] = mask_sel(s[i], bits, 8 * (i / 4) + (i % 4));
+            }
+            float x[16], sum[4];
+            auto weigh = [&](int from, int to) {
+#pragma unroll
+              for (int i = from; i < to; ++i) {
+                const float e = exp2_fast(__builtin_fmaf(s[i], p.c_log2, -r.m[0]));
+                asm volatile("" : : "v"(e));  // (here, not where it is used: the compiler gathers what it may behind the fences)
+                x[i] = e;
+                sum[i % 4] = i < 4 ? e : sum[i % 4] + e;
+              }
+            };
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+              s_next = mfma32(kf[i % 2], r.q[0][i], i == 0 ? zero16() : s_next);
+              if (i + 2 < kSteps) kf[i % 2] = frag_nat<D>(k_tile(1 - b), nat, 0, i + 2);
+              weigh(2 * i, 2 * i + 2);
+              if (i % (kSteps * PARTS / 8) == 0) put_share(kr[b], k_tile(b), mine, i / (kSteps * PARTS / 8));
+              __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int db = 0; db < kFrags; ++db) vf[0][db] = frag_tr<D>(v_tile(b), off4.tr, 0, db);
+            load(kr[b], u + 4, k_pages, k_scale);
+            const float limit = __builtin_amdgcn_ballot_w64(any_far != 0) != 0 ? kNearLimit : kFarLimit;
+            float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(total > limit) != 0, 0)) {
+              const float mx = max_halves(max16(s)) * p.c_log2;
+              const bool need = max_halves(total) > limit && mx > r.m[0];
+              const float m_new = need ? mx : r.m[0], alpha = exp2_fast(r.m[0] - m_new);
+              r.m[0] = m_new;
+              r.l[0] *= alpha;
+              r.w[0] *= alpha;
+#pragma unroll
+              for (int db = 0; db < kFrags; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) r.o[0][db][i] *= alpha;
+              weigh(0, 16);
+              total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            }
+            r.l[0] += total;
+            bf16x8 pb[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              u32x4 w;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                w[i] = pack_bf16(x[8 * t + 2 * i], x[8 * t + 2 * i + 1]);
+                r.w[0] = add_pair_bf16(w[i], r.w[0]);
+              }
+              pb[t] = __builtin_bit_cast(bf16x8, w);
+            }
+            keep_first(vr[1 - b], mine, keys_of(u + 1));
+            const int large = far_scale(vr[1 - b]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int db = 0; db < kFrags; ++db) vf[1][db] = frag_tr<D>(v_tile(b), off4.tr, 16, db);
+#pragma unroll
+            for (int k = 0; k < 2 * kFrags; ++k) {
+              r.o[0][k % kFrags] = mfma32(vf[k / kFrags][k % kFrags], pb[k / kFrags], r.o[0][k % kFrags]);
+              if (k % PARTS == 0) put_share(vr[1 - b], v_tile(1 - b), mine, k / PARTS);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            if (lane == 0) far[stream][1 - b][part] = large;
+            load(vr[1 - b], u + 3, v_pages, v_scale);
+          };
+          for (int u = 0; u < 2 * n; u += 2) {
+            turn(std::integral_constant<int, 0>(), u, sa, sb);
+            turn(std::integral_constant<int, 1>(), u + 1, sb, sa);
+          }
+        }
+        meet();  // (the tiles' last reads have left them)
+        first += 64;
+        if (first >= n_pages_0) break;
+        take_pages(first, 0);
+        continue;
+      }
       if constexpr (R::kPiped) {
         // A slot is a page, a page two turns.  Its second half is read when the first one's turn begins, and its slot filled again
         // when that has arrived.
