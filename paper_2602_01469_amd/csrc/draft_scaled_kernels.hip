@@ -640,9 +640,9 @@ __device__ __forceinline__ T* held(T* x) {  // (as a pointer to global memory, w
 }
 
 // A stream's share of LDS: a ring of slots of kTokens tokens each and, with codes of 4 bits, a tile for each of its waves.
-template <int D, CacheType T, int RB, int PARTS>
+template <int D, CacheType T, int RB, int PARTS, int WAVES, bool LONG>
 struct Ring {
-  static constexpr bool kSmall = D == 64 && RB == 1;                // four waves a SIMD, otherwise two
+  static constexpr bool kSmall = D == 64 && RB == 1 && !(kFour<T> && LONG);  // four waves a SIMD, otherwise two
   static constexpr int kRow = kFour<T> ? D / 2 : D;                 // bytes of a token's codes
   static constexpr int kSpace = (kSmall ? 8192 : 16384) * PARTS;    // codes of 8 bits: 128 KiB a CU
   static constexpr bool kShared = kFour<T> && D == 128 && PARTS == 4;  // waves with different rows widen each key once between them
@@ -667,10 +667,10 @@ struct Ring {
 // Bound: memory (64 requests of 8192 tokens: 102 us on MI355X with 24 rows of 128 features, 5.3 TB/s), with 56 rows of 64 features
 // vector issue beside it (121 us, 4.4 TB/s: 204 instructions a slot of 32 keys and 64 rows - a quarter of it exponentials - keep the vector
 // units busy for 64 % of a wave's time, the 16 matrix instructions theirs for 34 %).
-template <int D, CacheType T, int RB, int PARTS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_scaled_kernel(ScaledDecodeParams sp) {
+template <int D, CacheType T, int RB, int PARTS, int WAVES, bool LONG = false>
+__global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kSmall ? 4 : 2)) void draft_scaled_kernel(ScaledDecodeParams sp) {
   constexpr int kWaves = WAVES, kStreams = kWaves / PARTS;
-  using R = Ring<D, T, RB, PARTS>;
+  using R = Ring<D, T, RB, PARTS, WAVES, LONG>;
   constexpr int kTokens = R::kTokens, kHalf = R::kHalf, kSlot = R::kSlot, kDepth = R::kDepth, kRow = R::kRow;
   constexpr int kPerPage = kKeysPerTile / kTokens;                            // slots of a page
   constexpr int kCopies = R::kCopies;                                         // of a slot, by each of a stream's waves
@@ -1004,6 +1004,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
                 sum[i % 4] = i < 4 ? e : sum[i % 4] + e;
               }
             };
+            __builtin_amdgcn_s_setprio(1);  // (1 % here)
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
@@ -1015,6 +1016,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 && RB == 1 ? 4 : 2) void draft_
             }
 #pragma unroll
             for (int db = 0; db < kFrags; ++db) vf[0][db] = frag_tr<D>(v_tile(b), off4.tr, 0, db);
+            __builtin_amdgcn_s_setprio(0);
             load(kr[b], u + 4, k_pages, k_scale);
             const float limit = __builtin_amdgcn_ballot_w64(any_far != 0) != 0 ? kNearLimit : kFarLimit;
             float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -1371,13 +1373,17 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, CacheType c
   const dim3 grid((unsigned)(p.shares > 0 ? p.shares : p.d.C), (unsigned)p.d.Hkv);
   // With a workgroup a CU at most, two blocks of rows at D = 64 are two waves' rather than one's: what a wave does for a slot is
   // the time then (15.0 against 15.9 us for 4 requests of 2048 to 4096 tokens).  With more, widening each value once counts (91
-  // against 94 us for 64 of 512 to 8192).
+  // against 94 us for 64 of 512 to 8192).  With codes of 4 bits such a workgroup takes the turns that overlap where it has a whole request
+  // (20.4 us, otherwise 21.5, for 30 of 1000 to 2000 tokens), and not where it has a page or two a stream (15.0, otherwise 14.5, for 4 of
+  // 2048 to 4096).
   const bool alone = (int64_t)grid.x * grid.y <= kCus;
   auto go = [&](auto type) {
     constexpr CacheType T = decltype(type)::value;
+    constexpr bool four = T == CacheType::kE2M1;
     auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)waves * 64), 0, stream, p); };
     if (D == 64) {
       if (blocks == 1) run(draft_scaled_kernel<64, T, 1, 1, 8>, 8);
+      else if (blocks == 2 && alone && four && p.shares == 0) run(draft_scaled_kernel<64, T, 1, 2, 8, four>, 8);
       else if (blocks == 2 && alone) run(draft_scaled_kernel<64, T, 1, 2, 8>, 8);
       else if (blocks == 2) run(draft_scaled_kernel<64, T, 2, 1, 4>, 4);
       else run(draft_scaled_kernel<64, T, 2, 2, 4>, 4);

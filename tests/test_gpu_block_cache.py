@@ -440,7 +440,8 @@ def test_draft_matches_oracle(name, ctx_lens, K, Hq, Hkv, D):
 @pytest.mark.parametrize("C,ctx,K,Hq,Hkv,D", [(64, 20000, 2, 16, 8, 64), (64, 5000, 8, 128, 8, 128), (130, 9000, 4, 64, 4, 64), (256, 500, 7, 16, 2, 64),
                                               (70, 2000, 4, 8, 8, 128), (70, 900, 7, 32, 4, 64), (100, 2500, 7, 24, 4, 128), (40, 1500, 16, 64, 8, 64),
                                               (40, 6000, 4, 256, 8, 64), (64, 5000, 3, 16, 8, 128), (64, 4000, 8, 64, 4, 128), (40, 1500, 3, 32, 4, 128),
-                                              (50, 2000, 7, 32, 4, 128), (33, 1900, 16, 32, 4, 128)])
+                                              (50, 2000, 7, 32, 4, 128), (33, 1900, 16, 32, 4, 128),
+                                              (30, 2000, 7, 64, 8, 64), (20, 5000, 16, 32, 4, 128), (9, 300, 16, 32, 4, 128)])
 def test_draft_batches_on_a_shared_pool(C, ctx, K, Hq, Hkv, D):
     """Many requests whose tables point into a few pages: by request and in shares, one to four blocks of rows, more than 64 pages for
     a wave, unequal lengths; some of them against the oracle.  Then one request's table is spoiled: it alone is flagged and changes."""
