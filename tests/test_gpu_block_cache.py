@@ -406,7 +406,7 @@ class BlockRun(ScaledRun):
 
     def context(self, c):
         n = self.lens[c]
-        pages = torch.from_numpy(self.table[c, :-(-n // 64)].astype(np.int64)).cuda()
+        pages = torch.from_numpy(np.maximum(self.table[c, :-(-n // 64)], 0).astype(np.int64)).cuda()
         out = []
         for p, s in zip(self.pages, self.scales):
             x = orc.cache_values_blocks(_unpacked(p.view(torch.uint8)[pages]), s.view(torch.uint8)[pages].cpu().numpy())
@@ -461,9 +461,12 @@ def test_draft_batches_on_a_shared_pool(C, ctx, K, Hq, Hkv, D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-def test_draft_flags_bad_tables_and_lengths(D):
-    print(f"case block bad tables D={D}", flush=True)
-    r = BlockRun((300, 200, 100, 130, 64), 3, 8, 2, D, 3100)
+@pytest.mark.parametrize("K,Hq,Hkv", ROWS)
+def test_draft_flags_bad_tables_and_lengths(K, Hq, Hkv, D):
+    """Page ids on both sides of the pool, lengths below zero and beyond the table: flagged, skipped or clamped; what is left of such a
+    request, and the other requests, exact."""
+    print(f"case block bad tables K={K} Hq={Hq} D={D}", flush=True)
+    r = BlockRun((300, 200, 100, 130, 64), K, Hq, Hkv, D, 3100)
     good = r.run()
     r.bt[1, 2] = r.shape.n_pages + 5
     r.bt[3, 0] = -2**31
@@ -473,11 +476,42 @@ def test_draft_flags_bad_tables_and_lengths(D):
     o, lse, status = r.run()
     assert status.tolist() == [0, 1, 1, 1, 1] and np.array_equal(o[0], good[0][0]) and np.array_equal(lse[0], good[1][0])
     assert np.isfinite(lse[1:]).all()
-    k, v = r.context(1)                                       # (request 1: without the bad page's keys)
-    ro, rl = orc.draft_decode(*(bf16_bits_to_f64(x[1]) for x in r.host), np.delete(k, slice(128, 192), 0), np.delete(v, slice(128, 192), 0), r.shape.scale)
-    assert rel_l2(o[1], ro) <= REL and max_abs(lse[1], rl) <= LSE_ABS
-    ro, rl = orc.draft_decode(*(bf16_bits_to_f64(x[4]) for x in r.host), k[:0], v[:0], r.shape.scale)
-    assert rel_l2(o[4], ro) <= REL and max_abs(lse[4], rl) <= LSE_ABS
+    for c, bad in ((1, slice(128, 192)), (3, slice(0, 64)), (4, slice(0, None))):   # without the keys of the bad page, or any
+        k, v = (np.delete(x, bad, 0) for x in r.context(c))
+        ro, rl = orc.draft_decode(*(bf16_bits_to_f64(x[c]) for x in r.host), k, v, r.shape.scale)
+        assert rel_l2(o[c], ro) <= REL and max_abs(lse[c], rl) <= LSE_ABS, c
+
+
+@pytest.mark.parametrize("C,ctx,K,Hq,Hkv,D", [(256, 20000, 7, 64, 8, 64), (256, 20000, 2, 16, 8, 64), (256, 20000, 16, 64, 8, 64), (64, 20000, 8, 128, 8, 128),
+                                              (64, 20000, 7, 64, 8, 128), (128, 20000, 3, 64, 8, 128)])
+def test_draft_runs_of_more_pages_than_lanes(C, ctx, K, Hq, Hkv, D):
+    """Shares in which a wave has more than 64 pages of one request, whose ids a wave's lanes hold: two of the requests against the
+    oracle, and all of them the same twice."""
+    print(f"case block long runs C={C} K={K} Hq={Hq} D={D}", flush=True)
+    rng = np.random.default_rng(C + K)
+    lens = rng.integers(ctx // 2, ctx, C)
+    lens[1] = ctx
+    r = BlockRun(tuple(int(x) for x in lens), K, Hq, Hkv, D, C + K, shared=30)
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    r.check(o, lse, "long runs", (1, C // 2))
+    o2, lse2, _ = r.run()
+    assert np.array_equal(o, o2) and np.array_equal(lse, lse2)
+
+
+@pytest.mark.parametrize("K,Hq,D", [(2, 8, 64), (5, 8, 64), (16, 8, 64), (2, 8, 128), (5, 8, 128), (16, 8, 128)])
+def test_draft_of_more_than_a_thousand_requests(K, Hq, D):
+    """The first number of requests that take a workgroup each whatever they are long; one of them has more pages than lanes for every
+    stream."""
+    print(f"case block thousand K={K} D={D}", flush=True)
+    C = 1025
+    rng = np.random.default_rng(K)
+    lens = rng.integers(0, 150, C)
+    lens[0], lens[700] = 0, 40000
+    r = BlockRun(tuple(int(x) for x in lens), K, Hq, 1, D, 5000 + K, shared=30)
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    r.check(o, lse, "thousand", (0, 1, 500, 700, 701, C - 1))
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -690,6 +724,65 @@ def test_draft_on_tables_wider_than_any_context(C, ctx, columns, K, Hq, Hkv, D):
     o, lse, status = r.run()
     assert (status == 0).all()
     r.check(o, lse, "wide", range(0, C, max(1, C // 8)))
+
+
+def test_two_drafting_steps_at_once():
+    """Two streams, a workspace each: as one after the other."""
+    print("case block two streams", flush=True)
+    a, b = BlockRun((900, 70, 640, 2000), 7, 64, 8, 64, 4500), BlockRun((300, 1800), 8, 64, 4, 128, 4501)
+    want = a.run(), b.run()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for x, stream in zip((a, b), streams):
+        x.o.fill_(float("nan"))
+        stream.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for x, stream in zip((a, b), streams):
+            x.call(stream)
+    torch.cuda.synchronize()
+    for x, w in zip((a, b), want):
+        assert np.array_equal(bf16_to_f64(x.o), w[0]) and np.array_equal(x.lse.double().cpu().numpy(), w[1])
+
+
+def test_binding_says_what_is_wrong_with_a_call():
+    """Arguments that are not what the shape says are refused with their names before anything is launched; sizes may be any whole
+    numbers."""
+    print("case block binding", flush=True)
+    cache = Cache(np.random.default_rng(13), 3, 2, 64)
+    k = torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="cuda")
+    slots, shape = _slots_on(np.arange(5)), pe.CacheShape(5, 2, 64, 3)
+    pools = *cache.pages, *cache.scales
+    for call in (lambda s=shape, x=k, at=slots, p=pools: pe.peagle_cache_append_block_scaled(s, x, x, at, *p),
+                 lambda s=shape, x=k, at=slots, p=pools: pe.peagle_cache_read(s, at, *p, x, x)):
+        call()
+        call(s=pe.CacheShape(np.int64(5), np.int32(2), 64, 3))
+        for change, error, name in (({"x": k.float()}, TypeError, "k_"), ({"x": k[:4]}, ValueError, "k_"), ({"x": k.cpu()}, ValueError, "k_"),
+                                    ({"x": torch.zeros(5, 64, 2, dtype=torch.bfloat16, device="cuda").transpose(1, 2)}, ValueError, "k_"),
+                                    ({"at": slots.int()}, TypeError, "slots"), ({"at": slots[:3]}, ValueError, "slots"), ({"at": slots.cpu()}, ValueError, "slots"),
+                                    ({"p": (pools[0].view(torch.uint8), *pools[1:])}, TypeError, "k_pages"),
+                                    ({"p": (pools[0], pools[1][:2], *pools[2:])}, ValueError, "v_pages"),
+                                    ({"p": (*pools[:2], pools[2].view(torch.uint8), pools[3])}, TypeError, "k_scale"),
+                                    ({"p": (*pools[:3], pools[3].transpose(2, 3).contiguous())}, ValueError, "v_scale")):
+            with pytest.raises(error, match=name):
+                call(**change)
+        with pytest.raises(pe.PeagleError):
+            call(s=pe.CacheShape(5, 2, 64, 3), x=torch.zeros(5 * 132, dtype=torch.bfloat16, device="cuda").as_strided((5, 2, 64), (132, 64, 1)))
+    cache.check_read(np.arange(5, 192), "untouched")
+    r = BlockRun((70, 3), 3, 8, 2, 64, 4600)
+    good = r.run()
+    for name, x, error in (("q", r.q.float(), TypeError), ("k", r.k[:1], ValueError), ("o", r.o.transpose(1, 2).contiguous(), ValueError),
+                           ("bt", r.bt.long(), TypeError), ("cl", r.cl.cpu(), ValueError), ("lse", r.lse.half(), TypeError), ("ws", r.ws.int(), TypeError),
+                           ("status", r.status.long(), TypeError)):
+        kept = getattr(r, name)
+        setattr(r, name, x)
+        with pytest.raises(error):
+            r.call()
+        setattr(r, name, kept)
+    kept, r.ws = r.ws, r.ws[:16]
+    with pytest.raises(pe.PeagleError):
+        r.call()
+    r.ws = kept
+    again = r.run()
+    assert all(np.array_equal(x, y) for x, y in zip(good, again))
 
 
 def test_draft_equals_the_bf16_step_on_what_the_cache_reads_as():
