@@ -628,6 +628,8 @@ def _stream_on(device: int, stream):
     import torch
     if device != torch.cuda.current_device():
         raise ValueError(f"the tensors live on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError(f"the tensors live on cuda:{device}, the stream on cuda:{stream.device_index}")
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(device) if raw and stream is None else _stream_ptr(stream)
 

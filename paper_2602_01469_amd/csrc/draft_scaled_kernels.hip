@@ -7,7 +7,8 @@
 // infinite from 2^128 on): codes are widened to bf16, scale and all, by one instruction for two of them, between LDS and the
 // matrix instruction.  (The matrix instruction for 8-bit types, with queries split into two numbers of them, would need no widening
 // of keys, but its sums are not fp32 sums: 64 products of normal data came out 4e-5 of the largest sum off.)
-// The cache is read once, 2 Hkv D bytes a token, and bounds a large call; a small one is a chain of memory round trips.
+// The cache is read once, 2 Hkv D bytes a token (in 4 bits 17/16 Hkv D), and bounds a large call; a small one is a chain of memory
+// round trips.
 #include "attn_kernels.h"
 #include "attn_util.h"
 #include "cache_kernels.h"
@@ -283,7 +284,8 @@ __device__ __forceinline__ void cached_keys4(Rows<D, RB>& r, const char* k_at, c
 }
 
 // 32 keys in stages, for a wave that has two at work: while the vector unit turns the scores of one into probabilities, the matrix
-// unit multiplies the next one's keys.
+// unit multiplies the next one's keys.  (64 requests of 512 to 8192 tokens, 56 rows of 64 features: 68 us for a step, 73 with cached_keys4();
+// 48 of 500 to 8191, 128 rows of 128 features, 92 and 101.)
 template <int D>
 struct Keys4 {
   u32x4 k[D / 64], v[D / 64];
@@ -427,22 +429,22 @@ __device__ __forceinline__ void take4(Rows<D, RB>& r, f32x16 (&s)[RB], f32x16 (&
   }
 }
 
-// Several waves with different rows: each widens its share of 32 keys, and all of them read them as bf16 rows of two tiles of keys and
-// two of values, one of each being written while the other is read.
-template <int PARTS>
-struct Raw4 {  // a lane's share at D = 128: features of one key and block, and their scale
-  uint32_t w[8 / PARTS], scale;
+// Four waves with different rows: each widens a quarter of 32 keys, and all of them read them as bf16 rows of two tiles of keys and
+// two of values, one of each being written while the other is read.  Codes come from memory straight to registers, two turns before
+// they are widened.  (128 rows of 128 features: 84 us for a step of 48 requests of 500 to 8191 tokens, 92 where each wave widens all
+// keys.  Two waves that widen half of them each gain nothing.)
+struct Raw4 {  // a lane's share: sixteen features of one key, and their scale
+  u32x2 w;
+  uint32_t scale;
 };
-template <int PARTS>
 struct Share4 {
   int key, codes, scale;  // which key of 32; offsets of its codes and its scale
   int out;                // place of its first eight features in a tile
   __device__ __forceinline__ Share4(int part, int lane) {
     constexpr int D = 128;
-    const int i = lane & 7, block = PARTS == 2 ? lane >> 4 : (lane >> 3) & 3, half = PARTS == 2 ? 0 : lane >> 5;
+    const int i = lane & 7, block = (lane >> 3) & 3, half = lane >> 5;
     // (eight lanes that follow each other write to eight places modulo 128 bytes, as in value_key())
-    const int h = PARTS == 2 ? (lane >> 3) & 1 : part & 1;
-    key = (PARTS == 2 ? part : part >> 1) * 16 + (((i >> 1) << 2) | (h << 1) | (i & 1));
+    key = (part >> 1) * 16 + (((i >> 1) << 2) | ((part & 1) << 1) | (i & 1));
     codes = key * (D / 2) + block * 16 + half * 8;
     scale = key * (D / 32) + block;
     out = tile_off<D>(key, 4 * block + 2 * half);
@@ -454,33 +456,22 @@ __device__ __forceinline__ V load_global(const uint8_t* base, uint32_t off) {
   typedef const __attribute__((address_space(1))) uint8_t bytes;
   return *(const __attribute__((address_space(1))) V*)((bytes*)base + off);
 }
-template <int PARTS>
-__device__ __forceinline__ void load_share(Raw4<PARTS>& x, const uint8_t* codes, const uint8_t* scales, const Share4<PARTS>& mine) {
-  if constexpr (PARTS == 2) {
-    const u32x4 w = load_global<u32x4>(codes, (uint32_t)mine.codes);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.w[i] = w[i];
-  } else {
-    const u32x2 w = load_global<u32x2>(codes, (uint32_t)mine.codes);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) x.w[i] = w[i];
-  }
+__device__ __forceinline__ void load_share(Raw4& x, const uint8_t* codes, const uint8_t* scales, const Share4& mine) {
+  x.w = load_global<u32x2>(codes, (uint32_t)mine.codes);
   x.scale = load_global<uint8_t>(scales, (uint32_t)mine.scale);
 }
-template <int PARTS>
-__device__ __forceinline__ void put_share(const Raw4<PARTS>& x, char* tile, const Share4<PARTS>& mine, int i) {  // its eight features i
-  *reinterpret_cast<bf16x8*>(tile + (mine.out ^ (i << 4))) = widen4(x.w[i], __builtin_bit_cast(float, x.scale << 23));
+__device__ __forceinline__ void put_share(const Raw4& x, char* tile, const Share4& mine, int i) {  // its eight features i
+  const uint32_t word = x.w[i];
+  *reinterpret_cast<bf16x8*>(tile + (mine.out ^ (i << 4))) = widen4(word, __builtin_bit_cast(float, x.scale << 23));
 }
-template <int PARTS>
-__device__ __forceinline__ void keep_first(Raw4<PARTS>& x, const Share4<PARTS>& mine, int n) {  // zeros from key n on
+__device__ __forceinline__ void keep_first(Raw4& x, const Share4& mine, int n) {  // zeros from key n on
   if (n < 32) {
     x.scale = mine.key < n ? x.scale : 127u;
 #pragma unroll
-    for (int i = 0; i < 8 / PARTS; ++i) x.w[i] = mine.key < n ? x.w[i] : 0u;
+    for (int i = 0; i < 2; ++i) x.w[i] = mine.key < n ? x.w[i] : 0u;
   }
 }
-template <int PARTS>
-__device__ __forceinline__ bool far_scale(const Raw4<PARTS>& x) {
+__device__ __forceinline__ bool far_scale(const Raw4& x) {
   return __builtin_amdgcn_ballot_w64(x.scale > (uint32_t)kFarScale && x.scale != 255u) != 0;
 }
 // LDS of a workgroup whose waves share: all that it has written is there, and what it has read need not be any more.
@@ -639,7 +630,13 @@ __device__ __forceinline__ T* held(T* x) {  // (as a pointer to global memory, w
   return (T*)g;
 }
 
-// A stream's share of LDS: a ring of slots of kTokens tokens each and, with codes of 4 bits, a tile for each of its waves.
+// A stream's share of LDS: a ring of slots of kTokens tokens each and, with codes of 4 bits, a tile for each of its waves.  Codes of
+// 4 bits take one of three loops:
+//   kShared  128 rows of 128 features, four waves: put_share()
+//   kPiped   two waves a SIMD, whose registers hold two sets of scores: take4(); not at D = 128 with a wave a stream, for which slots
+//            of a whole page, as its two turns need them, would not fit
+//   else     cached_keys4(), where four waves a SIMD overlap each other's turns and where a stream is short (LONG: see the launch)
+// Two slots are enough for a page's turns: three and four gained nothing on either batch above.
 template <int D, CacheType T, int RB, int PARTS, int WAVES, bool LONG>
 struct Ring {
   static constexpr bool kSmall = D == 64 && RB == 1 && !(kFour<T> && LONG);  // four waves a SIMD, otherwise two
@@ -667,6 +664,10 @@ struct Ring {
 // Bound: memory (64 requests of 8192 tokens: 102 us on MI355X with 24 rows of 128 features, 5.3 TB/s), with 56 rows of 64 features
 // vector issue beside it (121 us, 4.4 TB/s: 204 instructions a slot of 32 keys and 64 rows - a quarter of it exponentials - keep the vector
 // units busy for 64 % of a wave's time, the 16 matrix instructions theirs for 34 %).
+// In 4 bits the bytes are half of that and the instructions as many, so that issue bounds a batch: 64 requests of 512 to 8192 tokens, 56
+// rows of 64 features, 70 us a step (2.3 TB/s), without any copies 10 % less; 48 of 500 to 8191, 128 rows of 128 features, 84 us (1.5 TB/s).  The
+// vector units are busy for 48 and 36 % of it, the matrix units for 23 and 26 %, and a wave waits for memory, LDS or a barrier 28 and
+// 30 % of its time; LDS conflicts are none.
 template <int D, CacheType T, int RB, int PARTS, int WAVES, bool LONG = false>
 __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kSmall ? 4 : 2)) void draft_scaled_kernel(ScaledDecodeParams sp) {
   constexpr int kWaves = WAVES, kStreams = kWaves / PARTS;
@@ -938,30 +939,30 @@ __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kS
     for (int first = 0;;) {
       if constexpr (R::kShared) {
         const int n = n_pages_0 - first < 64 ? n_pages_0 - first : 64;
-        const Share4<PARTS> mine(part, lane_id());
+        const Share4 mine(part, lane_id());
         const NatOff<D> nat = nat_offsets<D>(lane_id());
         char* const tiles = &ring[stream][0];
         auto k_tile = [&](int b) { return tiles + b * R::kTile; };
         auto v_tile = [&](int b) { return tiles + (2 + b) * R::kTile; };
-        auto load = [&](Raw4<PARTS>& x, int u, const uint8_t* pages, const uint8_t* scales) {  // of 32 keys u
+        auto load = [&](Raw4& x, int u, const uint8_t* pages, const uint8_t* scales) {  // of 32 keys u
           u = u < 2 * n ? u : u % 2;  // (always a load, so that what is under way can be counted)
           const size_t page_head = (size_t)(uint32_t)__builtin_amdgcn_readlane(page, u / 2) * p.Hkv + kvh;
           load_share(x, uniform_ptr(pages + page_head * (64 * kRow) + u % 2 * (32 * kRow)),
                      uniform_ptr(scales + page_head * (2 * D) + u % 2 * D), mine);
         };
         auto keys_of = [&](int u) { return __builtin_amdgcn_readlane(keys, u / 2) - u % 2 * 32; };
-        auto put = [&](const Raw4<PARTS>& x, char* to) {
+        auto put = [&](const Raw4& x, char* to) {
 #pragma unroll
-          for (int i = 0; i < 8 / PARTS; ++i) put_share(x, to, mine, i);
+          for (int i = 0; i < 2; ++i) put_share(x, to, mine, i);
         };
-        auto put_values = [&](Raw4<PARTS>& x, int u, int b) {
+        auto put_values = [&](Raw4& x, int u, int b) {
           keep_first(x, mine, keys_of(u));
           const int large = far_scale(x);
           put(x, v_tile(b));
           if (lane == 0) far[stream][b][part] = large;
         };
         if (n > 0) {
-          Raw4<PARTS> kr[2], vr[2];
+          Raw4 kr[2], vr[2];
           load(kr[0], 0, k_pages, k_scale);
           load(vr[0], 0, v_pages, v_scale);
           load(kr[1], 1, k_pages, k_scale);
@@ -1011,7 +1012,7 @@ __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kS
               s_next = mfma32(kf[i % 2], r.q[0][i], i == 0 ? zero16() : s_next);
               if (i + 2 < kSteps) kf[i % 2] = frag_nat<D>(k_tile(1 - b), nat, 0, i + 2);
               weigh(2 * i, 2 * i + 2);
-              if (i % (kSteps * PARTS / 8) == 0) put_share(kr[b], k_tile(b), mine, i / (kSteps * PARTS / 8));
+              if (i % (kSteps / 2) == 0) put_share(kr[b], k_tile(b), mine, i / (kSteps / 2));
               __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
@@ -1054,7 +1055,7 @@ __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kS
 #pragma unroll
             for (int k = 0; k < 2 * kFrags; ++k) {
               r.o[0][k % kFrags] = mfma32(vf[k / kFrags][k % kFrags], pb[k / kFrags], r.o[0][k % kFrags]);
-              if (k % PARTS == 0) put_share(vr[1 - b], v_tile(1 - b), mine, k / PARTS);
+              if (k % kFrags == 0) put_share(vr[1 - b], v_tile(1 - b), mine, k / kFrags);
               __builtin_amdgcn_sched_barrier(0);
             }
             if (lane == 0) far[stream][1 - b][part] = large;

@@ -17,7 +17,7 @@ namespace {
 decltype(&peagle_cache_append_block_scaled) g_append = nullptr;
 decltype(&peagle_cache_read) g_read = nullptr;
 decltype(&peagle_draft_decode_block_scaled) g_draft = nullptr;
-PyObject *s_n_tokens, *s_Hkv, *s_D, *s_n_pages, *s_C, *s_K, *s_Hq, *s_scale, *s_max_pages;
+PyObject *s_n_tokens, *s_Hkv, *s_D, *s_n_pages, *s_C, *s_K, *s_Hq, *s_scale, *s_max_pages, *s_device_index, *s_cuda_stream;
 
 struct Wrong {};  // an argument that the binding's checks have to look at
 
@@ -46,7 +46,8 @@ struct Call {
     if (stream_or_none == Py_None) {
       stream = (void*)c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream();
     } else {
-      PyObject* v = PyObject_GetAttrString(stream_or_none, "cuda_stream");
+      if (whole(stream_or_none, s_device_index) != device) throw Wrong();
+      PyObject* v = PyObject_GetAttr(stream_or_none, s_cuda_stream);
       if (!v) throw Wrong();
       stream = PyLong_AsVoidPtr(v);
       Py_DECREF(v);
@@ -91,6 +92,15 @@ struct Pools {
   }
 };
 
+// The library's entry points throw nothing; other threads may run meanwhile (a launch waits where the stream's queue is full).
+template <class F>
+int without_lock(F f) {
+  PyThreadState* const state = PyEval_SaveThread();
+  const int rc = f();
+  PyEval_RestoreThread(state);
+  return rc;
+}
+
 template <class F>
 PyObject* guarded(F f) {
   try {
@@ -121,7 +131,8 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     s.format = p.format;
     void* k = call.rows(a[1], shape, &s.k_stride);
     void* v = call.rows(a[2], shape, &s.v_stride);
-    return g_append(&s, k, v, (const int64_t*)call.whole_of(a[3], at::kLong, slots), p.k, p.v, p.ks, p.vs, call.stream);
+    const int64_t* at = (const int64_t*)call.whole_of(a[3], at::kLong, slots);
+    return without_lock([&] { return g_append(&s, k, v, at, p.k, p.v, p.ks, p.vs, call.stream); });
   });
 }
 
@@ -136,7 +147,8 @@ PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     s.format = p.format;
     void* k = call.rows(a[6], shape, &s.k_stride);
     void* v = call.rows(a[7], shape, &s.v_stride);
-    return g_read(&s, (const int64_t*)call.whole_of(a[1], at::kLong, slots), p.k, p.v, p.ks, p.vs, k, v, call.stream);
+    const int64_t* at = (const int64_t*)call.whole_of(a[1], at::kLong, slots);
+    return without_lock([&] { return g_read(&s, at, p.k, p.v, p.ks, p.vs, k, v, call.stream); });
   });
 }
 
@@ -165,10 +177,15 @@ PyObject* draft_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::ScalarType bf = at::kBFloat16, i32 = at::kInt;
     const at::Tensor& ws = tensor(a[13]);
     if (ws.scalar_type() != at::kByte || !ws.is_cuda() || ws.get_device() != call.device || !ws.is_contiguous()) throw Wrong();
-    return g_draft(&s, call.whole_of(a[1], bf, q), call.whole_of(a[2], bf, kv), call.whole_of(a[3], bf, kv), p.k, p.v, p.ks, p.vs,
-                   (const int32_t*)call.whole_of(a[8], i32, table), (const int32_t*)call.whole_of(a[9], i32, each), call.whole_of(a[10], bf, q),
-                   (float*)call.whole_of(a[11], at::kFloat, lse), a[12] == Py_None ? nullptr : (int32_t*)call.whole_of(a[12], i32, each),
-                   ws.data_ptr(), (size_t)ws.numel(), call.stream);
+    const void *q_new = call.whole_of(a[1], bf, q), *k_new = call.whole_of(a[2], bf, kv), *v_new = call.whole_of(a[3], bf, kv);
+    const int32_t *block_table = (const int32_t*)call.whole_of(a[8], i32, table), *ctx_len = (const int32_t*)call.whole_of(a[9], i32, each);
+    void *o = call.whole_of(a[10], bf, q), *sums = call.whole_of(a[11], at::kFloat, lse);
+    int32_t* status = a[12] == Py_None ? nullptr : (int32_t*)call.whole_of(a[12], i32, each);
+    void* workspace = ws.data_ptr();
+    const size_t ws_bytes = (size_t)ws.numel();
+    return without_lock([&] {
+      return g_draft(&s, q_new, k_new, v_new, p.k, p.v, p.ks, p.vs, block_table, ctx_len, o, (float*)sums, status, workspace, ws_bytes, call.stream);
+    });
   });
 }
 
@@ -204,7 +221,8 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     PyObject** to;
     const char* name;
   } names[] = {{&s_n_tokens, "n_tokens"}, {&s_Hkv, "Hkv"}, {&s_D, "D"},   {&s_n_pages, "n_pages"}, {&s_C, "C"},
-               {&s_K, "K"},               {&s_Hq, "Hq"},   {&s_scale, "scale"}, {&s_max_pages, "max_pages"}};
+               {&s_K, "K"},               {&s_Hq, "Hq"},   {&s_scale, "scale"}, {&s_max_pages, "max_pages"},
+               {&s_device_index, "device_index"}, {&s_cuda_stream, "cuda_stream"}};
   for (const auto& x : names)
     if (!(*x.to = PyUnicode_InternFromString(x.name))) return nullptr;
   return PyModule_Create(&module);

@@ -9,6 +9,8 @@ probabilities p (1 + d) weigh the values and are summed for the division: to fir
 here) by another 2e-3 sum p |v|, and by its own rounding, 2^-8 of itself.  In norm the roundings are random: one of them has a mean
 square of (2^-8 / sqrt 3)^2 times that of a significand's place in [1, 2), 1.7e-3 together, and the two of the probabilities and
 the output's are below 1.7e-3 * sqrt 3 = 2.9e-3 < 5e-3.  The LSE takes unrounded probabilities: off by what the scores are."""
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
@@ -173,6 +175,26 @@ def test_read_gives_a_slot_as_often_as_it_is_named():
     print("case block read repeats", flush=True)
     cache = Cache(np.random.default_rng(7), 3, 2, 128)
     cache.check_read(np.array([5] * 70 + [191, 0, 191]), "repeats")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_of_two_tokens_with_one_slot(D):
+    """Each piece of the slot is one of the two tokens'; nothing else is touched."""
+    print(f"case block one slot D={D}", flush=True)
+    rng = np.random.default_rng(77)
+    rows = torch.from_numpy(rng.standard_normal((40, 2, D))).bfloat16().cuda()
+    slots = np.arange(40) + 30
+    slots[37] = slots[2]                                      # (of other steps, waves)
+    slots[1] = slots[0]                                       # (of one step)
+    firsts, lasts = np.sort(np.unique(slots, return_index=True)[1]), 39 - np.sort(np.unique(slots[::-1], return_index=True)[1])
+    held = []
+    for keep in (np.arange(40), firsts, lasts):
+        cache = Cache(np.random.default_rng(5), 3, 2, D)
+        x = rows[torch.from_numpy(keep)]
+        pe.peagle_cache_append_block_scaled(pe.CacheShape(len(keep), 2, D, 3), x, x, _slots_on(slots[keep]), *cache.pages, *cache.scales)
+        held.append([x.view(torch.uint8).cpu().numpy() for x in (*cache.pages, *cache.scales)])
+    for both, a, b in zip(*held):
+        assert ((both == a) | (both == b)).all()
 
 
 def test_rows_that_stand_apart():
@@ -751,8 +773,8 @@ def test_binding_says_what_is_wrong_with_a_call():
     k = torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="cuda")
     slots, shape = _slots_on(np.arange(5)), pe.CacheShape(5, 2, 64, 3)
     pools = *cache.pages, *cache.scales
-    for call in (lambda s=shape, x=k, at=slots, p=pools: pe.peagle_cache_append_block_scaled(s, x, x, at, *p),
-                 lambda s=shape, x=k, at=slots, p=pools: pe.peagle_cache_read(s, at, *p, x, x)):
+    for call in (lambda s=shape, x=k, at=slots, p=pools, stream=None: pe.peagle_cache_append_block_scaled(s, x, x, at, *p, stream),
+                 lambda s=shape, x=k, at=slots, p=pools, stream=None: pe.peagle_cache_read(s, at, *p, x, x, stream)):
         call()
         call(s=pe.CacheShape(np.int64(5), np.int32(2), 64, 3))
         for change, error, name in (({"x": k.float()}, TypeError, "k_"), ({"x": k[:4]}, ValueError, "k_"), ({"x": k.cpu()}, ValueError, "k_"),
@@ -766,6 +788,9 @@ def test_binding_says_what_is_wrong_with_a_call():
                 call(**change)
         with pytest.raises(pe.PeagleError):
             call(s=pe.CacheShape(5, 2, 64, 3), x=torch.zeros(5 * 132, dtype=torch.bfloat16, device="cuda").as_strided((5, 2, 64), (132, 64, 1)))
+        with pytest.raises(ValueError, match="cuda:1"):
+            call(stream=SimpleNamespace(cuda_stream=torch.cuda.current_stream().cuda_stream, device_index=1))
+        call(stream=SimpleNamespace(cuda_stream=torch.cuda.current_stream().cuda_stream))
     cache.check_read(np.arange(5, 192), "untouched")
     r = BlockRun((70, 3), 3, 8, 2, 64, 4600)
     good = r.run()
