@@ -666,8 +666,8 @@ struct Ring {
 // units busy for 64 % of a wave's time, the 16 matrix instructions theirs for 34 %).
 // In 4 bits the bytes are half of that and the instructions as many, so that issue bounds a batch: 64 requests of 512 to 8192 tokens, 56
 // rows of 64 features, 70 us a step (2.3 TB/s), without any copies 10 % less; 48 of 500 to 8191, 128 rows of 128 features, 84 us (1.5 TB/s).  The
-// vector units are busy for 48 and 36 % of it, the matrix units for 23 and 26 %, and a wave waits for memory, LDS or a barrier 28 and
-// 30 % of its time; LDS conflicts are none.
+// vector units are busy for 60 and 47 % of the launch's cycles, the matrix units for 28 and 34 %, and a wave waits for memory, LDS or
+// a barrier 28 and 30 % of its time; LDS conflicts are none.
 template <int D, CacheType T, int RB, int PARTS, int WAVES, bool LONG = false>
 __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kSmall ? 4 : 2)) void draft_scaled_kernel(ScaledDecodeParams sp) {
   constexpr int kWaves = WAVES, kStreams = kWaves / PARTS;
