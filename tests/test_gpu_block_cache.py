@@ -9,6 +9,7 @@ probabilities p (1 + d) weigh the values and are summed for the division: to fir
 here) by another 2e-3 sum p |v|, and by its own rounding, 2^-8 of itself.  In norm the roundings are random: one of them has a mean
 square of (2^-8 / sqrt 3)^2 times that of a significand's place in [1, 2), 1.7e-3 together, and the two of the probabilities and
 the output's are below 1.7e-3 * sqrt 3 = 2.9e-3 < 5e-3.  The LSE takes unrounded probabilities: off by what the scores are."""
+import threading
 from types import SimpleNamespace
 
 import numpy as np
@@ -763,6 +764,47 @@ def test_two_drafting_steps_at_once():
     torch.cuda.synchronize()
     for x, w in zip((a, b), want):
         assert np.array_equal(bf16_to_f64(x.o), w[0]) and np.array_equal(x.lse.double().cpu().numpy(), w[1])
+
+
+def test_calls_from_two_threads():
+    """Each on a stream of its own, all three calls: as one after the other."""
+    print("case block two threads", flush=True)
+    runs = BlockRun((900, 70, 640, 2000), 7, 64, 8, 64, 4510), BlockRun((300, 1800), 8, 64, 4, 128, 4511)
+    want = [r.run() for r in runs]
+    rng = np.random.default_rng(19)
+    rows = [torch.from_numpy(rng.standard_normal((90, 4, D))).bfloat16().cuda() for D in (64, 128)]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            stream, D, r = torch.cuda.Stream(), (64, 128)[i], runs[i]
+            cache = Cache(np.random.default_rng(20 + i), 3, 4, D)
+            with torch.cuda.stream(stream):
+                k, v = torch.empty_like(rows[i]), torch.empty_like(rows[i])
+                for n in range(30):
+                    slots = _slots_on((np.arange(90) * 2 + n) % 192)
+                    shape = pe.CacheShape(90, 4, D, 3)
+                    pe.peagle_cache_append_block_scaled(shape, rows[i], rows[i], slots, *cache.pages, *cache.scales)
+                    pe.peagle_cache_read(shape, slots, *cache.pages, *cache.scales, k, v)
+                    r.call(stream)
+                stream.synchronize()
+            got[i] = k.clone(), v.clone(), bf16_to_f64(r.o), r.lse.double().cpu().numpy()
+        except Exception as e:  # noqa: BLE001  (shown by the assertion below)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not errors and all(g is not None for g in got), errors
+    for i, (k, v, o, lse) in enumerate(got):
+        held = np.zeros((2, 4, 64, (64, 128)[i]), np.int64), np.zeros((2, 4, 64, (64, 128)[i] // 32), np.int64)
+        orc.cache_append_blocks(bf16_to_f64(rows[i]), np.arange(90), *held)
+        ref = orc.cache_values_blocks(*held).transpose(0, 2, 1, 3).reshape(128, 4, -1)[:90]
+        assert np.array_equal(bf16_to_f64(k), ref) and np.array_equal(bf16_to_f64(v), ref)
+        assert np.array_equal(o, want[i][0]) and np.array_equal(lse, want[i][1])
 
 
 def test_binding_says_what_is_wrong_with_a_call():
