@@ -1238,11 +1238,13 @@ __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kS
 
 // Merges a request's partial records: M = max m_s, each sum and O the sum of the records' times 2^(m_s - M).  A row's threads - D / 4
 // for its features, LANES of them for the records in turn - look at EACH records at a time, whose loads are issued before the
-// first is used.
+// first is used.  With more LANES than a wave has for a row, four waves take it and are merged through LDS.
 template <int D, int LANES>
 constexpr int kMergeRows = 256 / (D / 4 * LANES);  // of a workgroup
 template <int D, int LANES, int EACH>
 __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeParams sp) {
+  constexpr int kWaveLanes = D / 4 * LANES > 64 ? 256 / D : LANES;  // of a row in one wave
+  static_assert(kWaveLanes == LANES || kMergeRows<D, LANES> == 1, "");
   const DecodeParams& p = sp.d;
   const int d4 = threadIdx.x % (D / 4), sl = threadIdx.x / (D / 4) % LANES;
   const int kvh = blockIdx.y, c = blockIdx.z, n_rows = p.K * p.group;
@@ -1288,7 +1290,7 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
     }
   }
 #pragma unroll
-  for (int x = D / 4; x < D / 4 * LANES; x <<= 1) {
+  for (int x = D / 4; x < D / 4 * kWaveLanes; x <<= 1) {
     const float m_other = __shfl_xor(M, x), m_new = __builtin_fmaxf(M, m_other);
     const float a = exp2_fast(M - m_new), b = exp2_fast(m_other - m_new);
     M = m_new;
@@ -1297,6 +1299,27 @@ __global__ __launch_bounds__(256) void draft_scaled_combine_kernel(ScaledDecodeP
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + __shfl_xor(acc[j], x) * b;
     bad |= __shfl_xor(bad, x);
+  }
+  if constexpr (kWaveLanes < LANES) {
+    __shared__ f32x4 sums[256 / 64], parts[256 / 64][D / 4];
+    const int wave = threadIdx.x >> 6;
+    if (sl % kWaveLanes == 0) {
+      parts[wave][d4] = acc;
+      if (d4 == 0) sums[wave] = f32x4{M, L, W, bad ? 1.f : 0.f};
+    }
+    __syncthreads();
+    if (sl != 0) return;
+#pragma unroll
+    for (int i = 1; i < 256 / 64; ++i) {
+      const f32x4 x = sums[i], o = parts[i][d4];
+      const float m_new = __builtin_fmaxf(M, x[0]), a = exp2_fast(M - m_new), b = exp2_fast(x[0] - m_new);
+      M = m_new;
+      L = L * a + x[1] * b;
+      W = W * a + x[2] * b;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + o[j] * b;
+      bad |= x[3] != 0.f;
+    }
   }
   if (sl != 0) return;
   if (p.status && row == 0 && kvh == 0 && d4 == 0) p.status[c] = bad;
@@ -1412,8 +1435,14 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, CacheType c
   // One thread for all of a row's records and four features where a request has a few records (64 requests of 512 to 8192 tokens, two or
   // three each: the step 79.8 us, 83.2 with four), otherwise four (D 64; two at D 128), or each would wait for more reads one after the
   // other (4 requests, nine each: 14.6, 15.1 with one).
-  const bool few = p.shares <= 4 * p.d.C;
-  if (D == 64) few ? merge(draft_scaled_combine_kernel<64, 1, 4>, kMergeRows<64, 1>) : merge(draft_scaled_combine_kernel<64, 4, 8>, kMergeRows<64, 4>);
+  // Four waves for a row, at codes of 4 bits, where the requests have 32 records and more in the mean, which a wave would read in two rounds and more:
+  // D 128, one of 12000 tokens 16.6 us, otherwise 19.9 (99 records, one KV head) and 15.7, 17.5 (50, four heads), 2 of 10800 to 20000
+  // 19.1, 20.3 (32, four heads); 4 of 9000 to 12000 17.3, 17.8 (32, two heads); D 64, 4 of 2000 to 9000 15.8, 16.2 (64, one head).  With
+  // fewer the waves' own merge costs more: 6 of 9000 to 12000 (D 64, 21 records, two heads) 15.5, otherwise 15.3, 4 of 2048 to 4096 15.5, 14.4.
+  const bool few = p.shares <= 4 * p.d.C, many = cache == CacheType::kE2M1 && p.shares >= 32 * p.d.C;
+  if (many && D == 64) merge(draft_scaled_combine_kernel<64, 16, 4>, kMergeRows<64, 16>);
+  else if (many) merge(draft_scaled_combine_kernel<128, 8, 8>, kMergeRows<128, 8>);
+  else if (D == 64) few ? merge(draft_scaled_combine_kernel<64, 1, 4>, kMergeRows<64, 1>) : merge(draft_scaled_combine_kernel<64, 4, 8>, kMergeRows<64, 4>);
   else few ? merge(draft_scaled_combine_kernel<128, 1, 4>, kMergeRows<128, 1>) : merge(draft_scaled_combine_kernel<128, 2, 16>, kMergeRows<128, 2>);
   return hipGetLastError();
 }

@@ -522,6 +522,28 @@ def test_draft_runs_of_more_pages_than_lanes(C, ctx, K, Hq, Hkv, D):
     assert np.array_equal(o, o2) and np.array_equal(lse, lse2)
 
 
+@pytest.mark.parametrize("lens,K,Hq,Hkv,D", [((40000,), 5, 16, 1, 128), ((12000,), 7, 8, 2, 128), ((10800, 20000), 5, 32, 4, 128), ((9000, 0, 70, 2000), 8, 16, 1, 64),
+                                             ((30000, 1), 3, 4, 1, 64), ((5000,), 64, 2, 1, 128), ((7000, 300, 8000), 1, 1, 1, 64)])
+def test_draft_of_many_records(lens, K, Hq, Hkv, D):
+    """Few long requests, whose merge four waves make for each row: up to 200 records a request, and requests of one or none.  A page
+    outside the pool, in the middle, is flagged, and its keys count for nothing."""
+    print(f"case block records {lens} K={K} Hq={Hq} D={D}", flush=True)
+    r = BlockRun(lens, K, Hq, Hkv, D, 5100 + K + len(lens))
+    o, lse, status = r.run()
+    assert (status == 0).all()
+    r.check(o, lse, "records")
+    o2, lse2, _ = r.run()
+    assert np.array_equal(o, o2) and np.array_equal(lse, lse2)
+    bad = -(-lens[0] // 64) // 2
+    r.bt[0, bad] = r.shape.n_pages
+    o2, lse2, status = r.run()
+    assert status.tolist() == [1] + [0] * (len(lens) - 1)
+    assert np.array_equal(o[1:], o2[1:]) and np.array_equal(lse[1:], lse2[1:])
+    k, v = (np.delete(x, slice(64 * bad, 64 * bad + 64), 0) for x in r.context(0))
+    ro, rl = orc.draft_decode(*(bf16_bits_to_f64(x[0]) for x in r.host), k, v, r.shape.scale)
+    assert rel_l2(o2[0], ro) <= REL and max_abs(lse2[0], rl) <= LSE_ABS
+
+
 @pytest.mark.parametrize("K,Hq,D", [(2, 8, 64), (5, 8, 64), (16, 8, 64), (2, 8, 128), (5, 8, 128), (16, 8, 128)])
 def test_draft_of_more_than_a_thousand_requests(K, Hq, D):
     """The first number of requests that take a workgroup each whatever they are long; one of them has more pages than lanes for every
