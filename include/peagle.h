@@ -518,7 +518,8 @@ int peagle_cache_append_block_scaled(const peagle_cache_shape_t* shape, const vo
  *   k_out, v_out     device, bf16 [n_tokens] rows of Hkv x D, 16-byte aligned (out; what stands between rows is left).  A token
  *                    whose slot is outside [0, 64 * n_pages) becomes zeros
  *
- * Codes times scales as the drafting steps widen them, exact wherever the product is a bf16 number.
+ * Codes times scales as the drafting steps widen them: exact wherever the product is a normal bf16 number, infinite from 2^128 on.
+ * Below the normal numbers (where the steps take it as zero) exact of 4 bits, off by up to 2^-126 of 8.
  */
 int peagle_cache_read(const peagle_cache_shape_t* shape, const int64_t* slots, const void* k_pages, const void* v_pages,
                       const void* k_scale, const void* v_scale, void* k_out, void* v_out, void* stream);

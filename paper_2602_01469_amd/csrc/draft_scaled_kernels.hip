@@ -1435,7 +1435,8 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, CacheType c
   // One thread for all of a row's records and four features where a request has a few records (64 requests of 512 to 8192 tokens, two or
   // three each: the step 79.8 us, 83.2 with four), otherwise four (D 64; two at D 128), or each would wait for more reads one after the
   // other (4 requests, nine each: 14.6, 15.1 with one).
-  // Four waves for a row, at codes of 4 bits, where the requests have 32 records and more in the mean, which a wave would read in two rounds and more:
+  // Four waves for a row, where the requests have 32 records and more in the mean, which a wave would read in two rounds and more (codes of
+  // 4 bits; with 8 a row's sums keep the order, and so the last bits, that they have had):
   // D 128, one of 12000 tokens 16.6 us, otherwise 19.9 (99 records, one KV head) and 15.7, 17.5 (50, four heads), 2 of 10800 to 20000
   // 19.1, 20.3 (32, four heads); 4 of 9000 to 12000 17.3, 17.8 (32, two heads); D 64, 4 of 2000 to 9000 15.8, 16.2 (64, one head).  With
   // fewer the waves' own merge costs more: 6 of 9000 to 12000 (D 64, 21 records, two heads) 15.5, otherwise 15.3, 4 of 2048 to 4096 15.5, 14.4.
