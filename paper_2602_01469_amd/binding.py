@@ -2,7 +2,9 @@
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
+import warnings
 from typing import Optional, Sequence
 
 import numpy as np
@@ -747,20 +749,34 @@ def peagle_draft_decode_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages,
         raise PeagleError(rc, "peagle_draft_decode_scaled")
 
 
+class _Unmarshalled:
+    """Stands where the compiled part of the binding cannot: every call takes the way through the checks here."""
+
+    @staticmethod
+    def _none(*_):
+        return None
+
+    cache_append = cache_read = draft_decode = _none
+
+
 def _fast():
     """The compiled part of the binding: its functions make a call whose arguments are all as they have to be and return the
-    status; of any other call they return None, and the checks here say what is wrong (or make it)."""
+    status; of any other call they return None, and the checks here say what is wrong (or make it).  Without it calls are the same
+    and take some 4 us longer, which is said once."""
     global _marshal
     if _marshal is None:
         import torch  # noqa: F401  (whose libraries it needs)
         lib = load_library()
         try:
             from . import _marshal as m
+            m.bind(*(C.cast(f, C.c_void_p).value for f in (lib.peagle_cache_append_block_scaled, lib.peagle_cache_read,
+                                                           lib.peagle_draft_decode_block_scaled)))
         except ImportError as e:
-            raise ImportError("_marshal.so is missing: build it with `python -m paper_2602_01469_amd.build` (or "
-                              "__graft_entry__.build())") from e
-        m.bind(*(C.cast(f, C.c_void_p).value for f in (lib.peagle_cache_append_block_scaled, lib.peagle_cache_read,
-                                                       lib.peagle_draft_decode_block_scaled)))
+            there = importlib.util.find_spec("._marshal", __package__) is not None
+            warnings.warn(("_marshal.so cannot be loaded (%s): rebuild it" % e if there else "_marshal.so is missing: build it") +
+                          " with `python -m paper_2602_01469_amd.build` (or __graft_entry__.build()); until then calls on 4-bit caches"
+                          " and reads are marshalled in Python", RuntimeWarning, stacklevel=3)
+            m = _Unmarshalled
         _marshal = m
     return _marshal
 
