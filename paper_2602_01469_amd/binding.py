@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
+import sys
 import warnings
 from typing import Optional, Sequence
 
@@ -749,6 +750,12 @@ def peagle_draft_decode_scaled(shape: DecodeShape, q_new, k_new, v_new, k_pages,
         raise PeagleError(rc, "peagle_draft_decode_scaled")
 
 
+def marshal_needs() -> str:
+    """The torch and the Python that this process runs, whose objects the compiled part of the binding reads."""
+    import torch
+    return f"torch {torch.__version__}, {sys.implementation.cache_tag}"
+
+
 class _Unmarshalled:
     """Stands where the compiled part of the binding cannot: every call takes the way through the checks here."""
 
@@ -769,6 +776,9 @@ def _fast():
         lib = load_library()
         try:
             from . import _marshal as m
+            built_for, needs = getattr(m, "built_for", "another torch"), marshal_needs()
+            if built_for != needs:
+                raise ImportError(f"built for {built_for}, this is {needs}")
             m.bind(*(C.cast(f, C.c_void_p).value for f in (lib.peagle_cache_append_block_scaled, lib.peagle_cache_read,
                                                            lib.peagle_draft_decode_block_scaled)))
         except ImportError as e:

@@ -27,8 +27,10 @@ def _run(cmd, what: str) -> str:
 
 def build_marshal() -> str:
     import torch
+    from .binding import marshal_needs
     torch_dir = os.path.dirname(torch.__file__)
-    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I" + os.path.join(torch_dir, "include"),
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", f'-DPEAGLE_BUILT_FOR="{marshal_needs()}"',
+          "-I" + os.path.join(torch_dir, "include"),
           "-I" + os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "-I/opt/rocm/include",
           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL, "-L" + os.path.join(torch_dir, "lib"),
           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"], "g++")

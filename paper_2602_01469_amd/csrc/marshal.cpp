@@ -3,6 +3,9 @@
 // Looking at a tensor from Python - its type, shape, strides, device and address - takes 0.4 us, seven of them as long as the GPU
 // takes for a small call; here all of them take 0.1 us.  A function returns the library's status, or None where an argument is not
 // what the call needs: the binding's own checks then say what is wrong.  Nothing is kept between calls.
+//
+// It reads tensors through torch's headers, whose layouts belong to one build of torch: `built_for` names that and the Python, and
+// the binding does without where they are others.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
@@ -225,5 +228,10 @@ PyMODINIT_FUNC PyInit__marshal(void) {
                {&s_device_index, "device_index"}, {&s_cuda_stream, "cuda_stream"}};
   for (const auto& x : names)
     if (!(*x.to = PyUnicode_InternFromString(x.name))) return nullptr;
-  return PyModule_Create(&module);
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", PEAGLE_BUILT_FOR) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
 }

@@ -51,6 +51,17 @@ def test_a_file_that_cannot_be_loaded_is_not_called_missing(folder):
     assert len(said) == 1
 
 
+def test_one_built_for_another_torch_is_not_used(monkeypatch):
+    """Its reads of tensors would be of another layout."""
+    if not os.path.exists(os.path.join(os.path.dirname(pe.__file__), "_marshal.so")):
+        pytest.skip("not built")
+    monkeypatch.setattr(binding, "_marshal", None)
+    monkeypatch.setattr(torch, "__version__", "1.0.0")
+    with pytest.warns(RuntimeWarning, match=r"cannot be loaded \(built for torch .*, this is torch 1.0.0, .*\): rebuild"):
+        _refused_by_the_checks()
+    assert binding._marshal is not sys.modules[pe.__name__ + "._marshal"]
+
+
 def test_the_built_one_is_taken():
     if not os.path.exists(os.path.join(os.path.dirname(pe.__file__), "_marshal.so")):
         pytest.skip("not built")
