@@ -8,6 +8,7 @@ import torch
 
 import paper_2602_01469_amd as pe
 from paper_2602_01469_amd import binding
+from paper_2602_01469_amd import build as _build
 
 F4, E8M0, BF16 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu, torch.bfloat16
 
@@ -49,6 +50,23 @@ def test_a_file_that_cannot_be_loaded_is_not_called_missing(folder):
     with pytest.warns(RuntimeWarning, match=r"_marshal.so cannot be loaded \(.*_marshal.so.*\): rebuild") as said:
         _refused_by_the_checks()
     assert len(said) == 1
+
+
+@pytest.mark.parametrize("error", [RuntimeError("g++ failed"), FileNotFoundError("g++"), ImportError("torch")])
+def test_the_library_is_built_without_it(monkeypatch, tmp_path, error):
+    """A build without a host compiler, torch or its headers ends with the library, and leaves no older compiled part beside it."""
+    def run(cmd, what):
+        if what == "g++":
+            raise error
+        return ""
+
+    old = tmp_path / "_marshal.so"
+    old.write_bytes(b"older")
+    monkeypatch.setattr(_build, "_run", run)
+    monkeypatch.setattr(_build, "MARSHAL", str(old))
+    with pytest.warns(RuntimeWarning, match="_marshal.so is not built"):
+        assert _build.build() == _build.LIB
+    assert not old.exists()
 
 
 def test_one_built_for_another_torch_is_not_used(monkeypatch):
