@@ -26,16 +26,16 @@ def _run(cmd, what: str) -> str:
     return out
 
 
-def build_marshal() -> str:
+def build_marshal(out: str = "", compiler: str = "g++", flags: tuple = ("-O2",)) -> str:
     import torch
     from .binding import marshal_needs
     torch_dir = os.path.dirname(torch.__file__)
-    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", f'-DPEAGLE_BUILT_FOR="{marshal_needs()}"',
+    _run([compiler, *flags, "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", f'-DPEAGLE_BUILT_FOR="{marshal_needs()}"',
           "-I" + os.path.join(torch_dir, "include"),
           "-I" + os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "-I/opt/rocm/include",
-          "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL, "-L" + os.path.join(torch_dir, "lib"),
-          "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"], "g++")
-    return MARSHAL
+          "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", out or MARSHAL, "-L" + os.path.join(torch_dir, "lib"),
+          "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"], compiler)
+    return out or MARSHAL
 
 
 def build(verbose: bool = False, sanitize_host_to: str = "") -> str:
