@@ -466,9 +466,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache_append_blocks_kernel(Row
   }
 }
 
-// Rows leave past the caches, which they would fill for nothing: 139 k tokens of 8 heads of 64 features, 4 bits, 53.6 us, otherwise
-// 87.0 (their codes come out of the last cache in part there); 13701 tokens 6.3, otherwise 7.9.
-template <int D, CacheType T>
+// PAST: the rows leave past the caches (see the launch).
+template <int D, CacheType T, bool PAST>
 __global__ __launch_bounds__(kRowWaves * 64) void cache_read_kernel(RowsParams p) {
   using L = RowLane<D>;
   constexpr bool kFour = T == CacheType::kE2M1;
@@ -524,7 +523,9 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache_read_kernel(RowsParams p
       put(2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false));
       put(3, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true));
     }
-    __builtin_nontemporal_store(out, reinterpret_cast<u32x4*>(rows + t * stride));
+    u32x4* row = reinterpret_cast<u32x4*>(rows + t * stride);
+    if (PAST) __builtin_nontemporal_store(out, row);
+    else *row = out;
   }
 }
 
@@ -546,12 +547,25 @@ hipError_t launch_cache_append_blocks(const RowsParams& p, int D, hipStream_t st
   return hipGetLastError();
 }
 
+// What is read is for a kernel that comes next: rows that the last cache (256 MiB) can hold for it stay there, others leave past it.
+// Read and a copy of the rows, 8 heads of 64 features, 4 bits: 28 MB of rows 18.3 us (20.4 from codes that no cache holds), past the
+// caches 20.7 (23.7), though the read by itself takes 7.8 instead of 6.1; 61 MB 32.7, past 37.5; 75 MB 45.1 and 45.3; 95 MB 65.3,
+// past 63.3; 134 MB 94.5, past 91.0; 285 MB 195, past 188, and the read by itself 84 instead of 53.  (What only reads the rows gains
+// from keeping them at each of these sizes: 5 to 8 % of both up to 134 MB, 2 % at 285.)
+constexpr int64_t kKeptRows = 72ll << 20;  // bytes of K and V
+
 hipError_t launch_cache_read(const RowsParams& p, int D, CacheType cache, hipStream_t stream) {
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows_grid(p, D), dim3(kRowWaves * 64), 0, stream, p); };
+  const bool past = (int64_t)p.n_tokens * p.Hkv * D * 4 > kKeptRows;
+  auto go = [&](auto type) {
+    constexpr CacheType T = decltype(type)::value;
+    if (D == 64) past ? run(cache_read_kernel<64, T, true>) : run(cache_read_kernel<64, T, false>);
+    else past ? run(cache_read_kernel<128, T, true>) : run(cache_read_kernel<128, T, false>);
+  };
   switch (cache) {
-    case CacheType::kE4M3: D == 64 ? run(cache_read_kernel<64, CacheType::kE4M3>) : run(cache_read_kernel<128, CacheType::kE4M3>); break;
-    case CacheType::kE5M2: D == 64 ? run(cache_read_kernel<64, CacheType::kE5M2>) : run(cache_read_kernel<128, CacheType::kE5M2>); break;
-    case CacheType::kE2M1: D == 64 ? run(cache_read_kernel<64, CacheType::kE2M1>) : run(cache_read_kernel<128, CacheType::kE2M1>); break;
+    case CacheType::kE4M3: go(std::integral_constant<CacheType, CacheType::kE4M3>()); break;
+    case CacheType::kE5M2: go(std::integral_constant<CacheType, CacheType::kE5M2>()); break;
+    case CacheType::kE2M1: go(std::integral_constant<CacheType, CacheType::kE2M1>()); break;
   }
   return hipGetLastError();
 }
