@@ -537,11 +537,16 @@ dim3 rows_grid(const RowsParams& p, int D) {
 
 }  // namespace
 
+// Bytes of K and V rows that one kernel leaves in the last cache for the next.
+constexpr int64_t kKeptRows = 72ll << 20;
+
 hipError_t launch_cache_append_blocks(const RowsParams& p, int D, hipStream_t stream) {
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows_grid(p, D), dim3(kRowWaves * 64), 0, stream, p); };
-  // Rows that fill half of the last cache (256 MiB) are read past it: 266 MB 60.6 us, 64.9 otherwise; 41 MB that it holds from what
-  // has written them 9.9, 12.8 past it.
-  const bool large = (int64_t)p.n_tokens * p.Hkv * D * 4 > 128ll << 20;
+  // Rows that the last cache (256 MiB) holds from the kernel that has written them are read from it, others past it.  That kernel (a
+  // copy) and the append, D 64, past the cache and otherwise: 41 MB 24.2 and 24.0 us, 58 MB 31.5 and 31.1, 72 MB 37.5 and 37.2, 78 MB 39.9 and
+  // 41.5, 90 MB 45.3 and 52.6, 110 MB 60.0 and 74.0, 128 MB 72.2 and 80.9, 266 MB 161 and 168; D 128 alike.  (Rows that nothing has written since the
+  // cache took them are faster from it up to 110 MB, 25.9 against 30.2.)
+  const bool large = (int64_t)p.n_tokens * p.Hkv * D * 4 > kKeptRows;
   if (D == 64) large ? run(cache_append_blocks_kernel<64, true>) : run(cache_append_blocks_kernel<64, false>);
   else large ? run(cache_append_blocks_kernel<128, true>) : run(cache_append_blocks_kernel<128, false>);
   return hipGetLastError();
@@ -552,8 +557,6 @@ hipError_t launch_cache_append_blocks(const RowsParams& p, int D, hipStream_t st
 // caches 20.7 (23.7), though the read by itself takes 7.8 instead of 6.1; 61 MB 32.7, past 37.5; 75 MB 45.1 and 45.3; 95 MB 65.3,
 // past 63.3; 134 MB 94.5, past 91.0; 285 MB 195, past 188, and the read by itself 84 instead of 53.  (What only reads the rows gains
 // from keeping them at each of these sizes: 5 to 8 % of both up to 134 MB, 2 % at 285.)
-constexpr int64_t kKeptRows = 72ll << 20;  // bytes of K and V
-
 hipError_t launch_cache_read(const RowsParams& p, int D, CacheType cache, hipStream_t stream) {
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows_grid(p, D), dim3(kRowWaves * 64), 0, stream, p); };
   const bool past = (int64_t)p.n_tokens * p.Hkv * D * 4 > kKeptRows;
