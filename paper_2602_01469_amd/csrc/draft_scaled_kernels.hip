@@ -7,8 +7,8 @@
 // infinite from 2^128 on): codes are widened to bf16, scale and all, by one instruction for two of them, between LDS and the
 // matrix instruction.  (The matrix instruction for 8-bit types, with queries split into two numbers of them, would need no widening
 // of keys, but its sums are not fp32 sums: 64 products of normal data came out 4e-5 of the largest sum off.)
-// The cache is read once, 2 Hkv D bytes a token (in 4 bits 17/16 Hkv D), and bounds a large call; a small one is a chain of memory
-// round trips.
+// The cache is read once, 2 Hkv D bytes a token, and bounds a large call on 8 bits.  In 4 bits a token has 17/16 Hkv D bytes, and no unit
+// alone bounds a large call (below).  A small one is a chain of memory round trips.
 #include "attn_kernels.h"
 #include "attn_util.h"
 #include "cache_kernels.h"
@@ -664,10 +664,10 @@ struct Ring {
 // Bound: memory (64 requests of 8192 tokens: 102 us on MI355X with 24 rows of 128 features, 5.3 TB/s), with 56 rows of 64 features
 // vector issue beside it (121 us, 4.4 TB/s: 204 instructions a slot of 32 keys and 64 rows - a quarter of it exponentials - keep the vector
 // units busy for 64 % of a wave's time, the 16 matrix instructions theirs for 34 %).
-// In 4 bits the bytes are half of that and the instructions as many, so that issue bounds a batch: 64 requests of 512 to 8192 tokens, 56
-// rows of 64 features, 70 us a step (2.3 TB/s), without any copies 10 % less; 48 of 500 to 8191, 128 rows of 128 features, 84 us (1.5 TB/s).  The
-// vector units are busy for 60 and 47 % of the launch's cycles, the matrix units for 28 and 34 %, and a wave waits for memory, LDS or
-// a barrier 28 and 30 % of its time; LDS conflicts are none.
+// In 4 bits the bytes are half of that and the instructions as many, and no unit alone bounds a batch.  64 requests of 512 to 8192 tokens,
+// 56 rows of 64 features: 67 us a step (2.3 TB/s), without any copies 10 % less; 48 of 500 to 8191, 128 rows of 128 features: 83 us (1.5 TB/s).  Of
+// the launch's cycles the vector units are busy for 60 and 46 %, the matrix units for 28 and 34 %; its waves are there for 86 and 96 % (starts,
+// unequal ends), and wait for memory, LDS or a barrier 28 and 30 % of that, for issue 24 and 30 %; LDS conflicts are none.
 template <int D, CacheType T, int RB, int PARTS, int WAVES, bool LONG = false>
 __global__ __launch_bounds__(WAVES * 64, (Ring<D, T, RB, PARTS, WAVES, LONG>::kSmall ? 4 : 2)) void draft_scaled_kernel(ScaledDecodeParams sp) {
   constexpr int kWaves = WAVES, kStreams = kWaves / PARTS;
@@ -1339,7 +1339,8 @@ constexpr int kCus = 256;  // compute units of the device
 // How the work of a KV head is shared, from the sizes that the host knows; times as microseconds a step on MI355X, D 64, 8 heads
 // of keys, 7 or 8 rows a position unless noted.
 //   lead   the start of a request's part (table, queries, merge) takes as long as some 8 pages: with 4 or 16 4 requests of 2048 to
-//          4096 take 16.6 or 15.3 instead of 14.7, 48 of 500 to 8191 (D 128, 128 rows) 95.8 or 96.3 instead of 91.
+//          4096 take 16.6 or 15.3 instead of 14.7, 48 of 500 to 8191 (D 128, 128 rows) 95.8 or 96.3 instead of 91.  (On 4 bits, where a page
+//          takes less, 12 would be better by up to 5 % for nine of twelve sizes, and worse by 1, 1 and 6 % for three.)
 //   least  two pages a stream, so that each wave has copies under way while it works.
 //   By request, without the second launch: where one request's pages are too few to divide (at most two a stream), and where
 //          eight a stream or fewer meet half the CUs' worth of workgroups: 14.8 against 21.1 for 16 requests of 1000 tokens, 22.0
@@ -1359,7 +1360,8 @@ constexpr int kCus = 256;  // compute units of the device
 //          difference with several.  A long request among short ones pays for it: 135 against 57 for one of 20000 among 1500 of 100 to 1000.
 // The rule sees the table's width; lengths are on the device.  In a table wider than they need, shares and their merge are taken where
 // a workgroup for each request would be faster: with 320 columns 17.7 instead of 12.5 for 16 of 1000, 26.3 instead of 18.8 for 32 of
-// 1000 to 2000, 17.7 instead of 13.6 for 4 of 2048 to 4096 (two workgroups a CU instead of one); nothing for 64 of 512 to 8192.
+// 1000 to 2000, 17.7 instead of 13.6 for 4 of 2048 to 4096 (two workgroups a CU instead of one); nothing for 64 of 512 to 8192.  (4 bits:
+// 18.8 instead of 13.6, 26.4 instead of 20.2, 18.1 instead of 14.8, nothing.)
 ShareRule draft_scaled_rule(int C, int Hkv, int max_pages, int blocks, int D) {
   ShareRule r;
   r.waves = D == 64 && blocks == 1 ? 8 : 4;
@@ -1435,8 +1437,10 @@ hipError_t launch_draft_scaled(const ScaledDecodeParams& pin, int D, CacheType c
   // One thread for all of a row's records and four features where a request has a few records (64 requests of 512 to 8192 tokens, two or
   // three each: the step 79.8 us, 83.2 with four), otherwise four (D 64; two at D 128), or each would wait for more reads one after the
   // other (4 requests, nine each: 14.6, 15.1 with one).
-  // Four waves for a row, where the requests have 32 records and more in the mean, which a wave would read in two rounds and more (codes of
-  // 4 bits; with 8 a row's sums keep the order, and so the last bits, that they have had):
+  // Four waves for a row, where the table leaves room for 32 records and more a request, which a wave would read in two rounds and more (codes
+  // of 4 bits; with 8 a row's sums keep the order, and so the last bits, that they have had).  Lengths, and with them how many records there
+  // are, only the device knows: with two or three in tables of 320 columns either merge takes as long (eight steps of 12 to 15 us, 0.15 apart
+  // at most).  With the tables' width full:
   // D 128, one of 12000 tokens 16.6 us, otherwise 19.9 (99 records, one KV head) and 15.7, 17.5 (50, four heads), 2 of 10800 to 20000
   // 19.1, 20.3 (32, four heads); 4 of 9000 to 12000 17.3, 17.8 (32, two heads); D 64, 4 of 2000 to 9000 15.8, 16.2 (64, one head).  With
   // fewer the waves' own merge costs more: 6 of 9000 to 12000 (D 64, 21 records, two heads) 15.5, otherwise 15.3, 4 of 2048 to 4096 15.5, 14.4.
